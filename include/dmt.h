@@ -29,6 +29,14 @@
  * For callers that can neither allocate nor hand over a workspace:
  *   dmt_tower_lookup_bwd_update_noalloc   the update on a scratch array that
  *                                lives inside the library
+ * For a branch of the model that reads a user's history item by item and answers
+ * with the next one (no plan; plain tensors with row strides):
+ *   dmt_embed_fwd, dmt_embed_bwd   rows by id, scaled, one per id; the table's
+ *                                gradient, summed by id, in dense form
+ *   dmt_layer_norm_fwd, dmt_layer_norm_bwd   layer norm, its gradients
+ *   dmt_token_logprob_fwd, dmt_token_logprob_bwd   log probabilities of given
+ *                                items, entropy, the top k; the scores' gradient
+ *   dmt_grad_norm, dmt_grad_clip   2-norm over many gradients, clipping to it
  *
  * Conventions
  *  - C linkage, no exceptions cross the boundary; every call returns dmt_status.
@@ -478,6 +486,136 @@ dmt_status dmt_sptt_peer_permute_ids(const int32_t* indices, const int64_t* offs
  * (features, peers) transposed and flattened as (peers x features). */
 dmt_status dmt_sptt_shuffle(const void* in, void* out, int64_t features, int64_t peers,
                             int64_t block_bytes, void* stream);
+
+/*
+ * ------------------------------------------------------------------ the sequence branch
+ *
+ * The calls below take plain row-major matrices: `x_stride` and the like are the elements from
+ * one row to the next (at least the row's own, any value, so a column range of a wider tensor
+ * is a matrix too), rows may start at any element, and sizes and strides are 64 bits wide
+ * (offsets may pass 2^32).  Pointers are dev and aligned to their element.  No plan is needed.
+ * Arithmetic is float32 whatever the types, every output is rounded once, sums have a fixed order (results repeat
+ * bit for bit).  Empty matrices are accepted.  Workspaces are the caller's, 256-byte aligned,
+ * need no initialisation and hold nothing between calls.
+ *
+ * first_bad, where a call takes it: dev int64 or NULL.  The caller sets it to -1; a call lowers
+ * it to the smallest position of an id or target >= the table's rows (of the scores' columns).
+ * Such an entry is skipped like a negative one, which stands for "none here" and is not reported.
+ */
+
+/*
+ * Rows of a table by id, one output row per id (no pooling), scaled:
+ *   out[i][c] = scale * table[ids[i]][c];  zeros where ids[i] is negative or >= rows.
+ *   table  [rows][cols] of table_dtype; ids dev int32 [n]; out [n][cols] of out_dtype
+ * rows >= 1, cols >= 1, n >= 0; DMT_ENOTSUP for n or rows beyond 2^31 - 1, cols beyond 2^24.
+ */
+dmt_status dmt_embed_fwd(const void* table, int64_t rows, int64_t cols, int64_t table_stride,
+                         int32_t table_dtype, const int32_t* ids, int64_t n, float scale, void* out,
+                         int64_t out_stride, int32_t out_dtype, int64_t* first_bad, void* stream);
+
+/*
+ * The table's gradient of dmt_embed_fwd, dense, float32:
+ *   grad_table[v][c] = scale * sum over i with ids[i] = v, ascending i in a fixed grouping, of grad[i][c]
+ * Every row is written, those that no id names with zeros; with accumulate != 0 the sum is added
+ * to what the row holds and rows that no id names are not touched (further micro-batches, a table used twice).
+ *   grad   [n][cols] of grad_dtype; grad_table [rows][cols] float32
+ */
+size_t dmt_embed_bwd_workspace_bytes(int64_t n, int64_t rows, int64_t cols);
+dmt_status dmt_embed_bwd(const int32_t* ids, int64_t n, const void* grad, int64_t grad_stride,
+                         int32_t grad_dtype, float scale, float* grad_table, int64_t rows,
+                         int64_t cols, int64_t grad_table_stride, int32_t accumulate,
+                         int64_t* first_bad, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Layer norm over rows:  mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps),
+ *   y = (x - mean) * rstd * gamma + beta
+ *   x, y         [rows][cols] of dtype; y may be x itself (same stride)
+ *   gamma, beta  [cols] of weight_dtype (dtype or DMT_F32); either may be NULL (1, 0)
+ *   mean, rstd   float32 [rows] out, what the backward reads; either may be NULL
+ * cols >= 1, rows >= 0; DMT_ENOTSUP for cols beyond 2^24 or rows beyond 2^31 - 1.
+ */
+dmt_status dmt_layer_norm_fwd(const void* x, int64_t rows, int64_t cols, int64_t x_stride,
+                              int32_t dtype, const void* gamma, const void* beta,
+                              int32_t weight_dtype, float eps, void* y, int64_t y_stride, float* mean,
+                              float* rstd, void* stream);
+
+/*
+ * Its gradients.  With h = (x - mean) * rstd and g = dy * gamma:
+ *   dx = rstd * (g - mean_c(g) - h * mean_c(g * h)),  dgamma = sum_rows dy * h,  dbeta = sum_rows dy
+ *   dy, dx         [rows][cols] of grad_dtype (dtype or DMT_F32); dx may be dy itself (same stride)
+ *   dgamma, dbeta  float32 [cols], overwritten; either may be NULL
+ *   workspace      dmt_layer_norm_bwd_workspace_bytes(rows, cols); may be NULL when both are NULL
+ */
+size_t dmt_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+dmt_status dmt_layer_norm_bwd(const void* x, int64_t rows, int64_t cols, int64_t x_stride,
+                              int32_t dtype, const void* gamma, int32_t weight_dtype,
+                              const float* mean, const float* rstd, const void* dy, int64_t dy_stride,
+                              int32_t grad_dtype, void* dx, int64_t dx_stride, float* dgamma,
+                              float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * What a row of scores over `vocab` items says, as the distribution p = softmax(x):
+ *   logprob[r]  = log p[targets[r]]; 0 where the target is negative or >= vocab
+ *   entropy[r]  = - sum_j p_j log p_j
+ *   top_ids[r][0..k), top_logprobs[r][0..k)   the k largest scores, ties by the lower item; -1 and
+ *                 -inf behind the last item that there is
+ *   stats[r]    = { max_j x_j, sum_j exp(x_j - max) }, what the backward reads
+ * A score of -inf is masked: it takes no part in anything (a masked target has logprob -inf).  A row
+ * whose mask leaves nothing has logprob -inf (0 without a target), entropy 0, no top items, stats {-inf, 0} and no gradient.
+ * A row that holds a NaN or +inf has NaN for logprob and entropy; its top items are some items of
+ * the row, or -1.  Scores at the type's lowest finite value are ordinary scores.
+ *   x        [rows][vocab] of dtype;  targets dev int32 [rows], NULL when logprob is
+ *   logprob, entropy  float32 [rows];  stats float32 [rows][2];  top_ids int32 [rows][k],
+ *            top_logprobs float32 [rows][k];  any of them may be NULL (top_logprobs needs top_ids)
+ *   k        0 ... DMT_TOP_MAX (0: no top items; may exceed vocab)
+ * vocab >= 1, rows >= 0; DMT_ENOTSUP for rows beyond 2^31 - 1 or vocab beyond 2^30.
+ */
+#define DMT_TOP_MAX 64
+size_t dmt_token_logprob_workspace_bytes(int64_t rows, int64_t vocab, int32_t k);
+dmt_status dmt_token_logprob_fwd(const void* x, int64_t rows, int64_t vocab, int64_t x_stride,
+                                 int32_t dtype, const int32_t* targets, float* logprob,
+                                 float* entropy, float* stats, int32_t k, int32_t* top_ids,
+                                 float* top_logprobs, int64_t* first_bad, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * The scores' gradient from the gradients of logprob and entropy (H), either of which may be NULL:
+ *   dx_j = grad_logprob * ([j = target] - p_j) - grad_entropy * p_j * (log p_j + H)
+ * Where there is no target the first term is 0.  Masked scores have gradient 0.
+ *   dx   [rows][vocab] of dtype; may be x itself (same stride)
+ *   stats as dmt_token_logprob_fwd wrote it; entropy likewise, needed with grad_entropy
+ */
+dmt_status dmt_token_logprob_bwd(const void* x, int64_t rows, int64_t vocab, int64_t x_stride,
+                                 int32_t dtype, const int32_t* targets, const float* stats,
+                                 const float* entropy, const float* grad_logprob,
+                                 const float* grad_entropy, void* dx, int64_t dx_stride, void* stream);
+
+/*
+ * The global 2-norm over many gradients, and clipping to it.
+ *   norm = sqrt(sum over all elements of g^2), the squares summed in float64: it neither overflows
+ *          nor vanishes where a float32 sum would
+ *   c    = min(1, max_norm / (norm + 1e-6));  out = c * g, rounded to the tensor's type
+ * A norm that is NaN makes every output NaN, an infinite one makes them 0 (NaN where g is
+ * infinite): the caller looks at `norm` to leave such a step out.
+ *   tensors  host [count], read during the call: `data` dev, contiguous, numel elements of dtype
+ *            (numel 0: data may be NULL); `out` dev of the same type and size, data itself
+ *            (in place) or memory that overlaps no gradient; ignored by dmt_grad_norm
+ *   norm     dev float32 [1] out; may be NULL for dmt_grad_clip
+ * In place with c = 1 nothing is written.  DMT_ENOTSUP beyond 2^20 tensors or 2^40 elements in one.
+ */
+typedef struct {
+  const void* data;
+  void* out;
+  int64_t numel;
+  int32_t dtype;
+  int32_t reserved; /* 0 */
+} dmt_grad_tensor;
+
+size_t dmt_grad_norm_workspace_bytes(const dmt_grad_tensor* tensors, int64_t count);
+dmt_status dmt_grad_norm(const dmt_grad_tensor* tensors, int64_t count, float* norm,
+                         void* workspace, size_t workspace_bytes, void* stream);
+dmt_status dmt_grad_clip(const dmt_grad_tensor* tensors, int64_t count, float max_norm, float* norm,
+                         void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Synchronise `stream` and report what the kernels since the last call found wrong with

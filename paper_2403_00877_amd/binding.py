@@ -48,6 +48,11 @@ class dmt_bwd_debug(ctypes.Structure):
                 ("num_unique", ctypes.c_void_p)]
 
 
+class dmt_grad_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class DmtError(RuntimeError):
     def __init__(self, where: str, code: int):
         self.code = code
@@ -106,6 +111,23 @@ def _load() -> ctypes.CDLL:
     lib.dmt_sptt_peer_permute.argtypes = [vp, vp, i64, i32, i32, i64, vp]
     lib.dmt_sptt_shuffle.argtypes = [vp, vp, i64, i64, i64, vp]
     lib.dmt_sptt_peer_permute_ids.argtypes = [vp, vp, i64, i32, i32, i64, i64, vp, vp, vp]
+    lib.dmt_embed_fwd.argtypes = [vp, i64, i64, i64, i32, vp, i64, f32, vp, i64, i32, vp, vp]
+    lib.dmt_embed_bwd_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.dmt_embed_bwd_workspace_bytes.restype = sz
+    lib.dmt_embed_bwd.argtypes = [vp, i64, vp, i64, i32, f32, vp, i64, i64, i64, i32, vp, vp, sz, vp]
+    lib.dmt_layer_norm_fwd.argtypes = [vp, i64, i64, i64, i32, vp, vp, i32, f32, vp, i64, vp, vp, vp]
+    lib.dmt_layer_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+    lib.dmt_layer_norm_bwd_workspace_bytes.restype = sz
+    lib.dmt_layer_norm_bwd.argtypes = [vp, i64, i64, i64, i32, vp, i32, vp, vp, vp, i64, i32, vp, i64, vp, vp,
+                                       vp, sz, vp]
+    lib.dmt_token_logprob_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.dmt_token_logprob_workspace_bytes.restype = sz
+    lib.dmt_token_logprob_fwd.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    lib.dmt_token_logprob_bwd.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.dmt_grad_norm_workspace_bytes.argtypes = [vp, i64]
+    lib.dmt_grad_norm_workspace_bytes.restype = sz
+    lib.dmt_grad_norm.argtypes = [vp, i64, vp, vp, sz, vp]
+    lib.dmt_grad_clip.argtypes = [vp, i64, f32, vp, vp, sz, vp]
     return lib
 
 
@@ -120,7 +142,11 @@ EXPORTS = ["dmt_status_str", "dmt_plan_create", "dmt_plan_destroy", "dmt_plan_la
            "dmt_calibration_copy", "dmt_calibration_gather", "dmt_tp_workspace_bytes", "dmt_tp_interaction",
            "dmt_tp_embed", "dmt_tp_kmeans", "dmt_sptt_peer_order", "dmt_sptt_peer_permute",
            "dmt_sptt_shuffle", "dmt_plan_set_row_shards", "dmt_bwd_noalloc_scratch_bytes",
-           "dmt_tower_lookup_bwd_update_noalloc", "dmt_sptt_peer_permute_ids"]
+           "dmt_tower_lookup_bwd_update_noalloc", "dmt_sptt_peer_permute_ids",
+           "dmt_embed_fwd", "dmt_embed_bwd_workspace_bytes", "dmt_embed_bwd", "dmt_layer_norm_fwd",
+           "dmt_layer_norm_bwd_workspace_bytes", "dmt_layer_norm_bwd", "dmt_token_logprob_workspace_bytes",
+           "dmt_token_logprob_fwd", "dmt_token_logprob_bwd", "dmt_grad_norm_workspace_bytes", "dmt_grad_norm",
+           "dmt_grad_clip"]
 
 DMT_K_COUNT = 15
 TP_STRATEGY_CODE = {"diverse": 0, "coherent": 1}
@@ -449,3 +475,159 @@ def dmt_plan_set_row_shards(plan: dmt_plan, row_begin: Sequence[int]) -> None:
     assert len(row_begin) == plan.num_tables
     arr = (ctypes.c_int64 * plan.num_tables)(*[int(r) for r in row_begin])
     _check("dmt_plan_set_row_shards", _lib.dmt_plan_set_row_shards(plan.handle, arr))
+
+
+# ---------------------------------------------------------------- the sequence branch
+#
+# Matrices are 2-D tensors whose last axis is contiguous; their row stride is handed over.  What the
+# library cannot see (a tensor too small, of another type, on the host) is checked here.
+
+def _rows(t: torch.Tensor, rows: int, cols: int, dtype=None) -> int:
+    """Row stride in elements of a [rows][cols] matrix."""
+    assert t.is_cuda and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols, (tuple(t.shape), rows, cols)
+    assert dtype is None or t.dtype == dtype, (t.dtype, dtype)
+    assert cols == 1 or t.stride(1) == 1, t.stride()
+    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _vec(t: Optional[torch.Tensor], n: int, dtype) -> None:
+    assert t is None or (t.is_cuda and t.is_contiguous() and t.numel() == n and t.dtype == dtype), \
+        (tuple(t.shape), t.dtype, n, dtype)
+
+
+def dmt_embed_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+                  first_bad: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out[i] = scale * table[ids[i]]; ids int32, any shape; out [ids.numel()][table's columns]."""
+    rows, cols = table.shape
+    n = ids.numel()
+    _vec(ids, n, torch.int32)
+    _vec(first_bad, 1, torch.int64)
+    _check("dmt_embed_fwd", _lib.dmt_embed_fwd(
+        _ptr(table), rows, cols, _rows(table, rows, cols), DTYPE_CODE[table.dtype], _ptr(ids), n, scale,
+        _ptr(out), _rows(out, n, cols), DTYPE_CODE[out.dtype], _ptr(first_bad), _stream(stream)))
+
+
+def dmt_embed_bwd_workspace_bytes(n: int, rows: int, cols: int) -> int:
+    return int(_lib.dmt_embed_bwd_workspace_bytes(n, rows, cols))
+
+
+def dmt_embed_bwd(ids: torch.Tensor, grad: torch.Tensor, grad_table: torch.Tensor, workspace: torch.Tensor,
+                  scale: float = 1.0, accumulate: bool = False, first_bad: Optional[torch.Tensor] = None,
+                  stream=None) -> None:
+    """grad_table (float32) = or += scale * the sum of grad's rows by id."""
+    rows, cols = grad_table.shape
+    n = ids.numel()
+    _vec(ids, n, torch.int32)
+    _vec(first_bad, 1, torch.int64)
+    _check("dmt_embed_bwd", _lib.dmt_embed_bwd(
+        _ptr(ids), n, _ptr(grad), _rows(grad, n, cols), DTYPE_CODE[grad.dtype], scale, _ptr(grad_table), rows,
+        cols, _rows(grad_table, rows, cols, torch.float32), int(accumulate), _ptr(first_bad), _ptr(workspace),
+        _nbytes(workspace), _stream(stream)))
+
+
+def _weight_code(x: torch.Tensor, *weights: Optional[torch.Tensor]) -> int:
+    types = {w.dtype for w in weights if w is not None}
+    assert len(types) <= 1, types
+    for w in weights:
+        if w is not None:
+            _vec(w, x.shape[1], w.dtype)
+    return DTYPE_CODE[types.pop()] if types else DMT_F32
+
+
+def dmt_layer_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
+                       y: torch.Tensor, mean: Optional[torch.Tensor] = None,
+                       rstd: Optional[torch.Tensor] = None, stream=None) -> None:
+    rows, cols = x.shape
+    _vec(mean, rows, torch.float32)
+    _vec(rstd, rows, torch.float32)
+    _check("dmt_layer_norm_fwd", _lib.dmt_layer_norm_fwd(
+        _ptr(x), rows, cols, _rows(x, rows, cols), DTYPE_CODE[x.dtype], _ptr(gamma), _ptr(beta),
+        _weight_code(x, gamma, beta), eps, _ptr(y), _rows(y, rows, cols, x.dtype), _ptr(mean), _ptr(rstd),
+        _stream(stream)))
+
+
+def dmt_layer_norm_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return int(_lib.dmt_layer_norm_bwd_workspace_bytes(rows, cols))
+
+
+def dmt_layer_norm_bwd(x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                       dy: torch.Tensor, dx: torch.Tensor, dgamma: Optional[torch.Tensor] = None,
+                       dbeta: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                       stream=None) -> None:
+    rows, cols = x.shape
+    for t, n in ((mean, rows), (rstd, rows), (dgamma, cols), (dbeta, cols)):
+        _vec(t, n, torch.float32)
+    _check("dmt_layer_norm_bwd", _lib.dmt_layer_norm_bwd(
+        _ptr(x), rows, cols, _rows(x, rows, cols), DTYPE_CODE[x.dtype], _ptr(gamma), _weight_code(x, gamma),
+        _ptr(mean), _ptr(rstd), _ptr(dy), _rows(dy, rows, cols), DTYPE_CODE[dy.dtype], _ptr(dx),
+        _rows(dx, rows, cols, dy.dtype), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), _nbytes(workspace),
+        _stream(stream)))
+
+
+def dmt_token_logprob_workspace_bytes(rows: int, vocab: int, k: int) -> int:
+    return int(_lib.dmt_token_logprob_workspace_bytes(rows, vocab, k))
+
+
+def dmt_token_logprob_fwd(x: torch.Tensor, targets: Optional[torch.Tensor] = None,
+                          logprob: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                          top_ids: Optional[torch.Tensor] = None, top_logprobs: Optional[torch.Tensor] = None,
+                          stats: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                          first_bad: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k is top_ids' second size."""
+    rows, vocab = x.shape
+    k = 0 if top_ids is None else top_ids.shape[1]
+    _vec(targets, rows, torch.int32)
+    _vec(logprob, rows, torch.float32)
+    _vec(entropy, rows, torch.float32)
+    _vec(stats, 2 * rows, torch.float32)
+    _vec(top_ids, rows * k, torch.int32)
+    _vec(top_logprobs, rows * k, torch.float32)
+    _vec(first_bad, 1, torch.int64)
+    _check("dmt_token_logprob_fwd", _lib.dmt_token_logprob_fwd(
+        _ptr(x), rows, vocab, _rows(x, rows, vocab), DTYPE_CODE[x.dtype], _ptr(targets), _ptr(logprob),
+        _ptr(entropy), _ptr(stats), k, _ptr(top_ids), _ptr(top_logprobs), _ptr(first_bad), _ptr(workspace),
+        _nbytes(workspace), _stream(stream)))
+
+
+def dmt_token_logprob_bwd(x: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor,
+                          entropy: Optional[torch.Tensor], grad_logprob: Optional[torch.Tensor],
+                          grad_entropy: Optional[torch.Tensor], dx: torch.Tensor, stream=None) -> None:
+    rows, vocab = x.shape
+    _vec(targets, rows, torch.int32)
+    _vec(stats, 2 * rows, torch.float32)
+    for t in (entropy, grad_logprob, grad_entropy):
+        _vec(t, rows, torch.float32)
+    _check("dmt_token_logprob_bwd", _lib.dmt_token_logprob_bwd(
+        _ptr(x), rows, vocab, _rows(x, rows, vocab), DTYPE_CODE[x.dtype], _ptr(targets), _ptr(stats),
+        _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(dx), _rows(dx, rows, vocab, x.dtype),
+        _stream(stream)))
+
+
+def make_grad_list(tensors: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None):
+    """The gradients' addresses and sizes, for dmt_grad_norm / dmt_grad_clip.  outs: where the clipped
+    gradients go (default: in place).  Returns a ctypes array; the tensors have to outlive its use."""
+    arr = (dmt_grad_tensor * len(tensors))()
+    outs = tensors if outs is None else outs
+    assert len(outs) == len(tensors)
+    for a, t, o in zip(arr, tensors, outs):
+        assert t.is_cuda and o.is_cuda and t.is_contiguous() and o.is_contiguous()
+        assert t.dtype == o.dtype and t.numel() == o.numel()
+        a.data, a.out, a.numel, a.dtype = t.data_ptr(), o.data_ptr(), t.numel(), DTYPE_CODE[t.dtype]
+    return arr
+
+
+def dmt_grad_norm_workspace_bytes(grad_list) -> int:
+    return int(_lib.dmt_grad_norm_workspace_bytes(grad_list, len(grad_list)))
+
+
+def dmt_grad_norm(grad_list, norm: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    _vec(norm, 1, torch.float32)
+    _check("dmt_grad_norm", _lib.dmt_grad_norm(grad_list, len(grad_list), _ptr(norm), _ptr(workspace),
+                                               _nbytes(workspace), _stream(stream)))
+
+
+def dmt_grad_clip(grad_list, max_norm: float, norm: Optional[torch.Tensor], workspace: torch.Tensor,
+                  stream=None) -> None:
+    _vec(norm, 1, torch.float32)
+    _check("dmt_grad_clip", _lib.dmt_grad_clip(grad_list, len(grad_list), max_norm, _ptr(norm), _ptr(workspace),
+                                               _nbytes(workspace), _stream(stream)))

@@ -1,0 +1,168 @@
+// Rows of matrices with any stride and alignment: pieces of up to 16 bytes a lane from any
+// element on, float32 values in between, one rounding on the way out.
+#pragma once
+
+#include "dmt_device_utils.h"
+
+namespace dmt {
+
+// gfx950 reads and writes a global 16-byte piece at any address; the types only tell the compiler
+// that an address is a multiple of the element alone.
+template <int EB> struct Piece;
+template <> struct Piece<4> {
+  typedef dmt_u32x4 __attribute__((aligned(4))) v4;
+  typedef dmt_u32x2 __attribute__((aligned(4))) v2;
+};
+template <> struct Piece<2> {
+  typedef dmt_u32x4 __attribute__((aligned(2))) v4;
+  typedef dmt_u32x2 __attribute__((aligned(2))) v2;
+};
+
+template <int DT> __device__ __forceinline__ uint32_t round2(float a, float b) {
+  if constexpr (DT == DMT_BF16) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    const dmt_f32x2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
+  } else {
+    return pack2<DT>(a, b);
+  }
+}
+
+template <int DT> __device__ __forceinline__ float load1(const char* p) {
+  if constexpr (DT == DMT_F32) {
+    return *(const DMT_GLOBAL float*)p;
+  } else {
+    const uint32_t u = *(const DMT_GLOBAL uint16_t*)p;
+    if constexpr (DT == DMT_BF16) return bf16_lo(u);
+    else return f16_bits_to_f32(u);
+  }
+}
+
+template <int DT> __device__ __forceinline__ void store1(char* p, float v) {
+  if constexpr (DT == DMT_F32) *(DMT_GLOBAL float*)p = v;
+  else *(DMT_GLOBAL uint16_t*)p = (uint16_t)round2<DT>(v, 0.f);
+}
+
+// Loads of weights whose type only the call knows.
+__device__ __forceinline__ float load1_dyn(const void* p, int64_t at, int dt) {
+  if (dt == DMT_F32) return load1<DMT_F32>((const char*)p + at * 4);
+  if (dt == DMT_F16) return load1<DMT_F16>((const char*)p + at * 2);
+  return load1<DMT_BF16>((const char*)p + at * 2);
+}
+
+// A lane's E consecutive elements as they lie in memory.
+template <int DT, int E> struct Raw {
+  static constexpr int kWords = E * EltBytes<DT>::value / 4;
+  uint32_t w[kWords];
+};
+
+// The first `valid` of them are there (valid >= 1 .. E; the others read as zero).
+template <int DT, int E>
+__device__ __forceinline__ Raw<DT, E> load_raw(const char* p, int valid) {
+  constexpr int EB = EltBytes<DT>::value, W = Raw<DT, E>::kWords;
+  Raw<DT, E> r;
+  if (valid >= E) {
+    if constexpr (W == 2) {
+      const dmt_u32x2 v = *(const DMT_GLOBAL typename Piece<EB>::v2*)p;
+      r.w[0] = v.x, r.w[1] = v.y;
+    } else {
+#pragma unroll
+      for (int q = 0; q < W; q += 4) {
+        const dmt_u32x4 v = *(const DMT_GLOBAL typename Piece<EB>::v4*)(p + q * 4);
+        r.w[q] = v.x, r.w[q + 1] = v.y, r.w[q + 2] = v.z, r.w[q + 3] = v.w;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < W; ++q) r.w[q] = 0;
+#pragma unroll
+    for (int i = 0; i < E - 1; ++i) {
+      if (i >= valid) break;
+      if constexpr (EB == 4) r.w[i] = *(const DMT_GLOBAL uint32_t*)(p + i * 4);
+      else r.w[i / 2] |= (uint32_t) * (const DMT_GLOBAL uint16_t*)(p + i * 2) << (i % 2 * 16);
+    }
+  }
+  return r;
+}
+
+template <int DT, int E>
+__device__ __forceinline__ void unpack(const Raw<DT, E>& r, float (&x)[E]) {
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    if constexpr (DT == DMT_F32) {
+      x[i] = __uint_as_float(r.w[i]);
+    } else {
+      float a, b;
+      unpack2<DT>(r.w[i / 2], a, b);
+      x[i] = i % 2 ? b : a;
+    }
+  }
+}
+
+template <int DT, int E>
+__device__ __forceinline__ void load_elems(const char* p, int valid, float (&x)[E]) {
+  unpack<DT, E>(load_raw<DT, E>(p, valid), x);
+}
+
+template <int DT, int E>
+__device__ __forceinline__ void store_elems(char* p, int valid, const float (&x)[E]) {
+  constexpr int EB = EltBytes<DT>::value, W = Raw<DT, E>::kWords;
+  if (valid >= E) {
+    uint32_t w[W];
+#pragma unroll
+    for (int q = 0; q < W; ++q) {
+      if constexpr (DT == DMT_F32) w[q] = __float_as_uint(x[q]);
+      else w[q] = round2<DT>(x[q * 2], x[q * 2 + 1]);
+    }
+    if constexpr (W == 2) {
+      const dmt_u32x2 v = {w[0], w[1]};
+      *(DMT_GLOBAL typename Piece<EB>::v2*)p = v;
+    } else {
+#pragma unroll
+      for (int q = 0; q < W; q += 4) {
+        const dmt_u32x4 v = {w[q], w[q + 1], w[q + 2], w[q + 3]};
+        *(DMT_GLOBAL typename Piece<EB>::v4*)(p + q * 4) = v;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E - 1; ++i) {
+      if (i >= valid) break;
+      store1<DT>(p + i * EB, x[i]);
+    }
+  }
+}
+
+// Sum over the lanes of an aligned group of G lanes, the same in each of them.
+template <int G> __device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+template <int G> __device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+
+// Sum over a block of NW waves, the same in every thread.  `smem` holds NW floats; ends with a barrier.
+template <int NW> __device__ __forceinline__ float block_sum(float v, float* smem) {
+  v = group_sum<64>(v);
+  if constexpr (NW == 1) return v;
+  if ((threadIdx.x & 63) == 0) smem[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float s = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) s += smem[w];
+  __syncthreads();
+  return s;
+}
+
+}  // namespace dmt
+
+// Host side: whether `dtype` is one of the three, and p aligned to it.
+static inline bool dmt_is_dtype(int32_t t) { return t == DMT_F32 || t == DMT_F16 || t == DMT_BF16; }
+static inline int64_t dmt_ebytes(int32_t t) { return t == DMT_F32 ? 4 : 2; }
+static inline bool dmt_is_at(const void* p, int64_t align) { return p && ((uintptr_t)p & (uintptr_t)(align - 1)) == 0; }
+// Whether an optional pointer is absent or aligned.
+static inline bool dmt_may_be_at(const void* p, int64_t align) { return ((uintptr_t)p & (uintptr_t)(align - 1)) == 0; }
