@@ -519,6 +519,7 @@ dmt_status dmt_embed_fwd(const void* table, int64_t rows, int64_t cols, int64_t 
  * Every row is written, those that no id names with zeros; with accumulate != 0 the sum is added
  * to what the row holds and rows that no id names are not touched (further micro-batches, a table used twice).
  *   grad   [n][cols] of grad_dtype; grad_table [rows][cols] float32
+ *   workspace of the size for (n, rows, cols); one sized for more ids serves fewer
  */
 size_t dmt_embed_bwd_workspace_bytes(int64_t n, int64_t rows, int64_t cols);
 dmt_status dmt_embed_bwd(const int32_t* ids, int64_t n, const void* grad, int64_t grad_stride,
