@@ -5,6 +5,7 @@
 // gradient row read once, and rows whose run spans tiles are joined from partial sums in a last launch.  One
 // writer per row, no atomics on values, every order fixed: the same bits every time.
 #include <algorithm>
+#include <type_traits>
 
 #include "dmt_internal.h"
 #include "dmt_rows.h"
@@ -43,6 +44,35 @@ __global__ __launch_bounds__(kBlock) void embed_fwd_kernel(
     }
     dmt::store_elems<OD, E>(dst + (int64_t)c * OB, valid, x);
   }
+}
+
+// ------------------------------------------------------------------ rows that no id names
+
+// They are cleared by waves of blocks behind those of the sums and of the join, which are bound by latency where the
+// clearing is bound by the rate of stores.
+struct Fill {
+  const uint8_t* touched;
+  float* out;
+  int64_t out_stride, rows;
+  int cols, log2_lanes, rows_per_wave;       // lanes that clear a row, rows a wave looks at (at most 64)
+  unsigned own_blocks;                       // the launch's blocks that do something else
+  int64_t first;                             // wave units cleared by earlier launches
+};
+constexpr int64_t kFillBytes = 16384, kFillWaves = 8192;   // of the table, cleared by a wave, while there are so many of them
+
+// Whether the block is one of those that clear rows; if so it is done.
+template <int Waves> __device__ __forceinline__ bool fill_block(const Fill& f) {
+  if (blockIdx.x < f.own_blocks) return false;
+  const int lane = threadIdx.x & 63, sub = lane & ((1 << f.log2_lanes) - 1);
+  const int64_t v0 = (f.first + (int64_t)(blockIdx.x - f.own_blocks) * Waves + (threadIdx.x >> 6)) * f.rows_per_wave;
+  const uint64_t empty = __ballot(lane < f.rows_per_wave && v0 + lane < f.rows && !f.touched[v0 + lane]);
+  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = lane >> f.log2_lanes; i < f.rows_per_wave; i += 64 >> f.log2_lanes) {
+    if (!(empty >> i & 1)) continue;
+    for (int c = sub * 4; c < f.cols; c += 4 << f.log2_lanes)
+      dmt::store_elems<DMT_F32, 4>((char*)(f.out + (v0 + i) * f.out_stride + c), min(4, f.cols - c), zero);
+  }
+  return true;
 }
 
 // ------------------------------------------------------------------ the lookups in order of their ids
@@ -87,23 +117,42 @@ __global__ __launch_bounds__(kSortBlock) void embed_digits(
   for (int d = threadIdx.x; d < nd; d += kSortBlock) counts[(int64_t)blockIdx.x * nd + d] = cnt[d];
 }
 
-// counts[block][digit] -> records of that digit in earlier blocks; totals[digit].
-__global__ __launch_bounds__(64) void embed_digit_starts(uint32_t* __restrict__ counts, int64_t nblk,
-                                                         int nd, uint32_t* __restrict__ totals) {
-  const int d = blockIdx.x * 64 + threadIdx.x;
-  if (d >= nd) return;
-  uint32_t run = 0;
-  for (int64_t b0 = 0; b0 < nblk; b0 += 16) {
-    uint32_t v[16];
+// counts[block][digit] -> records of that digit in earlier blocks; totals[digit].  A wave per 64 digits and sixteenth of the
+// blocks (one thread per digit over all the blocks was a chain of dependent batches: 9.6 us at 160 blocks, now 3.5).
+constexpr int kStartsSegs = 16, kStartsBatch = 16;
+__global__ __launch_bounds__(64 * kStartsSegs) void embed_digit_starts(uint32_t* __restrict__ counts, int64_t nblk,
+                                                                       int nd, uint32_t* __restrict__ totals) {
+  __shared__ uint32_t sums[kStartsSegs][64];
+  const int lane = threadIdx.x & 63, seg = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
+  const int64_t per = (nblk + kStartsSegs - 1) / kStartsSegs, b0 = seg * per, b1 = min(nblk, b0 + per);
+  uint32_t sum = 0, v[kStartsBatch];
+  if (d < nd)
+    for (int64_t b = b0; b < b1; b += kStartsBatch) {
 #pragma unroll
-    for (int u = 0; u < 16; ++u) v[u] = b0 + u < nblk ? counts[(b0 + u) * nd + d] : 0u;
+      for (int u = 0; u < kStartsBatch; ++u) v[u] = b + u < b1 ? counts[(b + u) * nd + d] : 0u;
 #pragma unroll
-    for (int u = 0; u < 16; ++u) {
-      if (b0 + u < nblk) counts[(b0 + u) * nd + d] = run;
-      run += v[u];
+      for (int u = 0; u < kStartsBatch; ++u) sum += v[u];
     }
+  sums[seg][lane] = sum;
+  __syncthreads();
+  uint32_t run = 0, all = 0;
+  for (int g = 0; g < kStartsSegs; ++g) {
+    run += g < seg ? sums[g][lane] : 0u;
+    all += sums[g][lane];
   }
-  totals[d] = run;
+  if (d >= nd) return;
+  if (seg == 0) totals[d] = all;
+  for (int64_t b = b0; b < b1; b += kStartsBatch) {
+    if (per > kStartsBatch)                  // (else they are still at hand)
+#pragma unroll
+      for (int u = 0; u < kStartsBatch; ++u) v[u] = b + u < b1 ? counts[(b + u) * nd + d] : 0u;
+#pragma unroll
+    for (int u = 0; u < kStartsBatch; ++u)
+      if (b + u < b1) {
+        counts[(b + u) * nd + d] = run;
+        run += v[u];
+      }
+  }
 }
 
 // Stable scatter.  A wave ranks 64 * items consecutive records, 64 at a time, by ballots of the digit's bits.
@@ -117,6 +166,15 @@ __global__ __launch_bounds__(kSortBlock) void embed_scatter(
   uint32_t* base = lds;                                   // [nd]
   uint16_t* mine = (uint16_t*)(lds + nd);                 // [waves][nd] records of the digit in this wave so far
   __shared__ uint32_t sm[kSortWaves];
+  const int64_t j0 = ((int64_t)blockIdx.x * kSortWaves + wave) * 64 * items + lane;
+  uint64_t rec[kMaxItems];
+  uint16_t rank[kMaxItems];
+#pragma unroll
+  for (int q = 0; q < kMaxItems; ++q)
+    if (q < items) {
+      const int64_t j = j0 + q * 64;
+      rec[q] = j < n ? record<First>(ids, in, j, rows) : ~0ull;
+    }
   for (int d = threadIdx.x; d < nd * kSortWaves / 2; d += kSortBlock) ((uint32_t*)mine)[d] = 0;
   // first record of each digit: a scan of the totals (two digits a thread at most), then the earlier blocks' share
   uint32_t before = 0;
@@ -128,15 +186,6 @@ __global__ __launch_bounds__(kSortBlock) void embed_scatter(
     before += all;
   }
   __syncthreads();
-  const int64_t j0 = ((int64_t)blockIdx.x * kSortWaves + wave) * 64 * items + lane;
-  uint64_t rec[kMaxItems];
-  uint16_t rank[kMaxItems];
-#pragma unroll
-  for (int q = 0; q < kMaxItems; ++q)
-    if (q < items) {
-      const int64_t j = j0 + q * 64;
-      rec[q] = j < n ? record<First>(ids, in, j, rows) : ~0ull;
-    }
 #pragma unroll
   for (int q = 0; q < kMaxItems; ++q)
     if (q < items) {
@@ -177,17 +226,17 @@ __global__ __launch_bounds__(kSortBlock) void embed_scatter(
     }
 }
 
-// Few lookups: the whole sort in one launch.  A block owns a range of rows and looks at every id itself, twice:
+// Few lookups: the whole order in one launch.  A block owns a range of rows and looks at every id itself, twice:
 // first it counts, per wave (a wave has a consecutive share of the ids) and row, and how many ids lie below its
 // range; then every id of the range has its place.  Counts are 16 bits, so n stays below 65536.
-constexpr int kFewRows = 4096;               // rows of a block, at most: counts of 16 waves take 128 KB
-constexpr int64_t kFewBlocks = 256;          // ... and the least number of blocks
-constexpr int64_t kFewNnz = 65535, kFewWork = 1 << 25;
+//   lds [waves][range / 2], two rows a word: afterwards where each wave's share of a row ends, counted from the
+//   block's first record;  counted(pair of rows, count of either) once per pair;
+//   placed(ids below the range, place, key, position) once per id of the range
 constexpr int kFewUnroll = 8;
-__global__ __launch_bounds__(kSortBlock) void embed_sort_few(
-    const int32_t* __restrict__ ids, int n, uint32_t rows, int range, uint64_t* __restrict__ out,
-    uint16_t* __restrict__ touched, unsigned long long* __restrict__ first_bad) {
-  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];        // [waves][range / 2], two rows a word
+template <typename Counted, typename Placed>
+__device__ __forceinline__ void order_few(const int32_t* __restrict__ ids, int n, uint32_t rows, int range, uint32_t* lds,
+                                              unsigned long long* __restrict__ first_bad, Counted counted,
+                                              Placed placed) {
   __shared__ uint32_t sm[kSortWaves];
   __shared__ uint32_t s_below;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, words = range / 2;
@@ -245,11 +294,10 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_few(
       const uint32_t add = (at & 0xffffu) | (at + a) << 16;             // (no place passes n)
 #pragma unroll
       for (int w = 0; w < kSortWaves; ++w) lds[w * words + p] = c[w] + add;
-      touched[first / 2 + p] = (uint16_t)((a > 0) | (b > 0) << 8);
+      counted(first / 2 + p, a, b);
     }
   }
   __syncthreads();
-  uint64_t* dst = out + s_below;
   uint16_t* place = (uint16_t*)mine;
   for (int j = j0; j < j1; j += kFewUnroll * 64) {
     uint32_t key[kFewUnroll];
@@ -266,7 +314,7 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_few(
         const uint32_t from = place[row];
         __builtin_amdgcn_wave_barrier();
         if (here && d == row) {
-          dst[from + __popcll(same & ((1ull << lane) - 1))] = (uint64_t)v << 32 | (uint32_t)at;
+          placed(s_below, from + __popcll(same & ((1ull << lane) - 1)), v, (uint32_t)at);
           place[row] = (uint16_t)(from + __popcll(same));               // (the same from every lane)
         }
         __builtin_amdgcn_wave_barrier();
@@ -276,14 +324,28 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_few(
   }
 }
 
+constexpr int kFewRows = 4096;               // rows of a block, at most: counts of 16 waves take 128 KB
+constexpr int64_t kFewBlocks = 256;          // ... and the least number of blocks
+constexpr int64_t kFewNnz = 65535, kFewWork = 1 << 25;
+__global__ __launch_bounds__(kSortBlock) void embed_sort_few(const int32_t* __restrict__ ids, int n, uint32_t rows, int range,
+                                                             uint64_t* __restrict__ out, uint16_t* __restrict__ touched,
+                                                             unsigned long long* __restrict__ first_bad) {
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  order_few(ids, n, rows, range, lds, first_bad,
+            [&](uint32_t pair, uint32_t a, uint32_t b) { touched[pair] = (uint16_t)((a > 0) | (b > 0) << 8); },
+            [&](uint32_t below, uint32_t place, uint32_t key, uint32_t at) {
+              out[below + place] = (uint64_t)key << 32 | at;
+            });
+}
+
 // ------------------------------------------------------------------ the sums
 
-// The sorted records are cut into tiles of equal length; a lane group walks one, with kUnroll gradient rows under way, and
-// writes a row when its run ends.  Runs that cross a tile's end leave partial sums: part[tile][0] of the
-// run that came from the tile before, part[tile][1] of one that starts here and goes on.  Blocks behind the
-// tiles' clear the rows that no id names.
+// The sorted records are cut into tiles of equal length; a lane group walks one, with kUnroll gradient rows under way,
+// and writes a row when its run ends.  A run belongs to the tile it starts in, whose group follows it into the next.  Only
+// long runs, those that hold the first records of two tiles, are shared: part[tile][0] is the sum of a long run
+// that came from the tile before, part[tile][1] of one that starts here and goes on, and embed_join adds them up.
+// kUnroll 16 took 91 us where 8 takes 61 (163840 lookups, with the clearing beside them): fewer waves fit.
 constexpr int kUnroll = 8;
-constexpr int kFillBytes = 65536;            // of the table, cleared by a block
 
 struct Sums {
   const uint64_t* recs;
@@ -294,134 +356,162 @@ struct Sums {
   float* out;
   int64_t out_stride;
   int cols, part_cols, accumulate, log2_lpr, tile;
-  int64_t ntiles, tile_blocks;
-  int slices;
+  int64_t ntiles;
+  int slices, log2_join;                     // log2 of the join's lanes per row
   float* part;
-  const uint8_t* touched;
-  int log2_fill;                             // lanes that clear a row, and rows a block looks at
-  int fill_rows;
+  Fill fill;
 };
 
 __device__ __forceinline__ uint32_t key_at(const uint64_t* recs, int64_t j) { return (uint32_t)(recs[j] >> 32); }
 
-template <int E>
+template <int E, bool Add>
 __device__ __forceinline__ void write_row(const Sums& a, uint32_t row, int c, int valid, float (&acc)[E]) {
   char* dst = (char*)(a.out + row * a.out_stride + c);
   float x[E];
-  if (a.accumulate) dmt::load_elems<DMT_F32, E>(dst, valid, x);
+  if (Add) dmt::load_elems<DMT_F32, E>(dst, valid, x);
 #pragma unroll
-  for (int q = 0; q < E; ++q) acc[q] = a.accumulate ? fmaf(a.scale, acc[q], x[q]) : a.scale * acc[q];
+  for (int q = 0; q < E; ++q) acc[q] = Add ? fmaf(a.scale, acc[q], x[q]) : a.scale * acc[q];
   dmt::store_elems<DMT_F32, E>(dst, valid, acc);
 }
 
-__device__ __forceinline__ void clear_rows(const Sums& a) {
-  const int lane = threadIdx.x & ((1 << a.log2_fill) - 1);
-  const int64_t v0 = (blockIdx.x - a.tile_blocks) * a.fill_rows, v1 = min(a.rows, v0 + a.fill_rows);
-  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t v = v0 + (threadIdx.x >> a.log2_fill); v < v1; v += kBlock >> a.log2_fill) {
-    if (a.touched[v]) continue;
-    for (int c = lane * 4; c < a.cols; c += 4 << a.log2_fill)
-      dmt::store_elems<DMT_F32, 4>((char*)(a.out + v * a.out_stride + c), min(4, a.cols - c), zero);
-  }
-}
-
-template <int GD>
+// Whole: every piece of a row is of E elements.  (A row may end at every one of the unrolled records, so what a row's end
+// does is in the code kUnroll times; without the paths of ragged pieces and of Add 63.3 -> 61.3 us.)
+template <int GD, bool Whole, bool Add>
 __global__ __launch_bounds__(kBlock) void embed_sums(const Sums a) {
   constexpr int E = dmt::ChunkElems<GD>::value, GB = dmt::EltBytes<GD>::value;
-  if (blockIdx.x >= a.tile_blocks) {
-    clear_rows(a);
-    return;
-  }
+  if (fill_block<kBlock / 64>(a.fill)) return;
   const int lane = threadIdx.x & ((1 << a.log2_lpr) - 1);
   const int64_t tile = (int64_t)(blockIdx.x / (unsigned)a.slices) * (kBlock >> a.log2_lpr) + (threadIdx.x >> a.log2_lpr);
   const int c = (int)((blockIdx.x % (unsigned)a.slices << a.log2_lpr) + lane) * E;
   if (tile >= a.ntiles || c >= a.cols) return;
-  const int valid = min(E, a.cols - c);
+  const int valid = Whole ? E : min(E, a.cols - c);
   const int64_t j0 = tile * a.tile, j1 = min(a.n, j0 + a.tile);
   const uint32_t rows = (uint32_t)a.rows;
-  const uint32_t prev = j0 > 0 ? key_at(a.recs, j0 - 1) : ~0u, next = j1 < a.n ? key_at(a.recs, j1) : ~0u;
+  // first records' keys of the tiles around this one, and the key before it
+  const uint32_t prev = j0 > 0 ? key_at(a.recs, j0 - 1) : ~0u, before = tile > 0 ? key_at(a.recs, j0 - a.tile) : ~0u;
+  const uint32_t first = key_at(a.recs, j0), last = key_at(a.recs, j1 - 1);
+  const uint32_t next = j1 < a.n ? key_at(a.recs, j1) : ~0u;
+  const uint32_t after = tile + 2 < a.ntiles ? key_at(a.recs, j1 + a.tile) : ~0u;
+  const bool long_in = first == prev && (before == first || next == first);
+  const bool long_out = last == next && (first == last || after == last);
+  const uint32_t skip = long_in ? ~0u : prev;              // a short run that came from the tile before is done there
   uint32_t cur = rows;
   float acc[E];
   auto flush = [&]() {
-    if (cur >= rows) return;
-    if (cur == prev || cur == next)
-      dmt::store_elems<DMT_F32, E>((char*)(a.part + (tile * 2 + (cur != prev)) * a.part_cols + c), E, acc);
-    else
-      write_row<E>(a, cur, c, valid, acc);
-  };
-  for (int64_t j = j0; j < j1; j += kUnroll) {
-    uint64_t rec[kUnroll];
-    dmt::Raw<GD, E> g[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) rec[u] = a.recs[min(j + u, j1 - 1)];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      g[u] = dmt::load_raw<GD, E>(a.grad + ((int64_t)(uint32_t)rec[u] * a.grad_stride + c) * GB, valid);
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (j + u >= j1) break;
-      const uint32_t key = (uint32_t)(rec[u] >> 32);
-      if (key != cur) {
-        flush();
-        cur = key;
-#pragma unroll
-        for (int q = 0; q < E; ++q) acc[q] = 0.f;
-      }
-      float x[E];
-      dmt::unpack<GD, E>(g[u], x);
-#pragma unroll
-      for (int q = 0; q < E; ++q) acc[q] += x[q];
+    if (cur >= rows || cur == skip) return;
+    const bool part = cur == prev || (cur == next && long_out);
+    if (Add && !part) {
+      write_row<E, true>(a, cur, c, valid, acc);
+      return;
     }
-  }
+    float* dst = part ? a.part + (tile * 2 + (cur != prev)) * a.part_cols + c : a.out + cur * a.out_stride + c;
+    const float f = part ? 1.f : a.scale;
+#pragma unroll
+    for (int q = 0; q < E; ++q) acc[q] *= f;
+    dmt::store_elems<DMT_F32, E>((char*)dst, part ? E : valid, acc);
+  };
+  // records j .. end - 1; past the tile's end only while they are the last run's
+  auto walk = [&](int64_t j, int64_t end, bool beyond) {
+    for (; j < end; j += kUnroll) {
+      uint64_t rec[kUnroll];
+      dmt::Raw<GD, E> g[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) rec[u] = a.recs[min(j + u, end - 1)];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint32_t key = (uint32_t)(rec[u] >> 32);
+        if (beyond ? key == cur : key != skip && key < rows)
+          g[u] = dmt::load_raw<GD, E>(a.grad + ((int64_t)(uint32_t)rec[u] * a.grad_stride + c) * GB, valid);
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (j + u >= end) break;
+        const uint32_t key = (uint32_t)(rec[u] >> 32);
+        if (key != cur) {
+          if (beyond) return;
+          flush();
+          cur = key;
+#pragma unroll
+          for (int q = 0; q < E; ++q) acc[q] = 0.f;
+        }
+        if (cur == skip || cur >= rows) continue;
+        float x[E];
+        dmt::unpack<GD, E>(g[u], x);
+#pragma unroll
+        for (int q = 0; q < E; ++q) acc[q] += x[q];
+      }
+    }
+  };
+  walk(j0, j1, false);
+  if (cur == next && cur != skip && cur < rows && !long_out) walk(j1, min(a.n, j1 + a.tile), true);
   flush();
 }
 
-// Rows whose run spans tiles: their partial sums, in the tiles' order.  A block looks at kJoinTiles tiles; each
+// Rows of long runs: their partial sums, in the tiles' order.  A block looks at kJoinTiles tiles; each
 // lane group takes the runs that start in one of them in turn, and the whole block those of many tiles.
-constexpr int kJoinTiles = 64, kJoinLong = 32;
-__global__ __launch_bounds__(kBlock) void embed_join(const Sums a) {
+constexpr int kJoinTiles = 64, kJoinLong = 16, kJoinBlock = 1024;
+
+// How many tiles from t + 1 on start with row v, tile t + 1 among them.  By a whole wave: 64 tiles, then every 64th ... of
+// them at a time, so a run of thousands of tiles takes a few reads after one another (bisection took twenty).
+__device__ __forceinline__ int64_t tiles_of_run(const Sums& a, int64_t t, uint32_t v) {
+  const int lane = threadIdx.x & 63;
+  int64_t good = t + 1, stride = 1;          // tile `good` starts with v
+  for (;;) {                                 // wider steps while all 64 do
+    const int64_t at = good + (lane + 1) * stride;
+    const bool is = at < a.ntiles && key_at(a.recs, at * a.tile) == v;
+    const int many = __builtin_popcountll(__ballot(is));     // (a prefix of the lanes: the records are sorted)
+    good += many * stride;
+    if (many == 64) {
+      stride *= 64;
+      continue;
+    }
+    if (stride == 1) return good - t;
+    stride /= 64;
+  }
+}
+
+template <bool Add>
+__global__ __launch_bounds__(kJoinBlock) void embed_join(const Sums a) {
   constexpr int E = 4;
   __shared__ int s_tile[kJoinTiles], s_len[kJoinTiles];
-  __shared__ int s_count;
-  __shared__ float s_sum[kBlock * E];
-  if (threadIdx.x == 0) s_count = 0;
-  __syncthreads();
+  __shared__ uint32_t s_row[kJoinTiles];
+  __shared__ float s_sum[kJoinBlock * E];
+  if (fill_block<kJoinBlock / 64>(a.fill)) return;
   const int64_t t0 = (int64_t)blockIdx.x * kJoinTiles;
-  if (threadIdx.x < kJoinTiles && t0 + (int)threadIdx.x + 1 < a.ntiles) {
-    const int64_t t = t0 + threadIdx.x, b = t * a.tile, e = b + a.tile;
-    const uint32_t v = key_at(a.recs, e - 1);
-    if ((int64_t)v < a.rows && key_at(a.recs, e) == v &&
-        (b == 0 || key_at(a.recs, b) != v || key_at(a.recs, b - 1) != v)) {
-      // the last tile that starts with the run: doubling steps, then bisection
-      int64_t good = t + 1, step = 1;
-      while (good + step < a.ntiles && key_at(a.recs, (good + step) * a.tile) == v) good += step, step *= 2;
-      int64_t bad = min(a.ntiles, good + step);
-      while (bad - good > 1) {
-        const int64_t mid = (good + bad) / 2;
-        if (key_at(a.recs, mid * a.tile) == v) good = mid;
-        else bad = mid;
-      }
-      const int at = atomicAdd(&s_count, 1);             // (which group takes which run changes no sum)
-      s_tile[at] = (int)threadIdx.x;
-      s_len[at] = (int)(good - t);
-    }
+  bool owns = false;
+  uint32_t row = 0;
+  if (t0 + (threadIdx.x & 63) + 1 < a.ntiles) {             // (every wave looks at all of the tiles)
+    const int64_t t = t0 + (threadIdx.x & 63), b = t * a.tile, e = b + a.tile;
+    const uint32_t v = key_at(a.recs, e - 1), next = key_at(a.recs, e), first = key_at(a.recs, b);
+    const uint32_t prev = b > 0 ? key_at(a.recs, b - 1) : ~0u, after = t + 2 < a.ntiles ? key_at(a.recs, e + a.tile) : ~0u;
+    owns = (int64_t)v < a.rows && next == v && (first != v || prev != v) && (first == v || after == v);
+    row = v;
+  }
+  const uint64_t starts = __ballot(owns);
+  const int count = __builtin_popcountll(starts);
+  if (count == 0) return;
+  uint64_t left = starts;
+  for (int i = 0; i < count; ++i, left &= left - 1) {
+    if (i % (kJoinBlock / 64) != threadIdx.x >> 6) continue;
+    const int at = __builtin_ctzll(left);
+    const uint32_t v = __builtin_amdgcn_readlane(row, at);
+    const int64_t many = tiles_of_run(a, t0 + at, v);
+    s_tile[i] = at;
+    s_row[i] = v;
+    s_len[i] = (int)many;
   }
   __syncthreads();
-  const int count = s_count, lane = threadIdx.x & ((1 << a.log2_fill) - 1);
-  const int group = threadIdx.x >> a.log2_fill, groups = kBlock >> a.log2_fill;
+  const int lane = threadIdx.x & ((1 << a.log2_join) - 1);
+  const int group = threadIdx.x >> a.log2_join, groups = kJoinBlock >> a.log2_join;
   auto heads = [&](int64_t t, int from, int to, int c, float (&acc)[E]) {
     const float* p = a.part + t * 2 * a.part_cols + c;
-    int i = from;
-    for (; i + 8 <= to; i += 8) {
+    for (int i = from; i < to; i += 8) {                    // (past the end: the last one again, not added)
       float4 x[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = *(const float4*)(p + (int64_t)(i + u) * 2 * a.part_cols);
+      for (int u = 0; u < 8; ++u) x[u] = *(const float4*)(p + (int64_t)min(i + u, to - 1) * 2 * a.part_cols);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) acc[0] += x[u].x, acc[1] += x[u].y, acc[2] += x[u].z, acc[3] += x[u].w;
-    }
-    for (; i < to; ++i) {
-      const float4 x = *(const float4*)(p + (int64_t)i * 2 * a.part_cols);
-      acc[0] += x.x, acc[1] += x.y, acc[2] += x.z, acc[3] += x.w;
+      for (int u = 0; u < 8; ++u)
+        if (i + u < to) acc[0] += x[u].x, acc[1] += x[u].y, acc[2] += x[u].z, acc[3] += x[u].w;
     }
   };
   auto tail = [&](int64_t t, int c, float (&acc)[E]) {
@@ -431,20 +521,20 @@ __global__ __launch_bounds__(kBlock) void embed_join(const Sums a) {
   for (int i = group; i < count; i += groups) {
     if (s_len[i] > kJoinLong) continue;
     const int64_t t = t0 + s_tile[i];
-    const uint32_t v = key_at(a.recs, (t + 1) * a.tile);
-    for (int c = lane * E; c < a.cols; c += E << a.log2_fill) {
+    const uint32_t v = s_row[i];
+    for (int c = lane * E; c < a.cols; c += E << a.log2_join) {
       float acc[E];
       tail(t, c, acc);
       heads(t, 1, s_len[i] + 1, c, acc);
-      write_row<E>(a, v, c, min(E, a.cols - c), acc);
+      write_row<E, Add>(a, v, c, min(E, a.cols - c), acc);
     }
   }
   for (int i = 0; i < count; ++i) {
     if (s_len[i] <= kJoinLong) continue;
     const int64_t t = t0 + s_tile[i];
-    const uint32_t v = key_at(a.recs, (t + 1) * a.tile);
+    const uint32_t v = s_row[i];
     const int per = (s_len[i] + groups - 1) / groups, from = 1 + group * per, to = min(s_len[i] + 1, from + per);
-    for (int c0 = 0; c0 < a.cols; c0 += E << a.log2_fill) {
+    for (int c0 = 0; c0 < a.cols; c0 += E << a.log2_join) {
       const int c = c0 + lane * E;
       float acc[E] = {0.f, 0.f, 0.f, 0.f};
       if (c < a.cols) heads(t, from, to, c, acc);
@@ -456,8 +546,95 @@ __global__ __launch_bounds__(kBlock) void embed_join(const Sums a) {
         tail(t, c, acc);
         for (int g = 0; g < groups; ++g)
 #pragma unroll
-          for (int q = 0; q < E; ++q) acc[q] += s_sum[((g << a.log2_fill) + lane) * E + q];
-        write_row<E>(a, v, c, min(E, a.cols - c), acc);
+          for (int q = 0; q < E; ++q) acc[q] += s_sum[((g << a.log2_join) + lane) * E + q];
+        write_row<E, Add>(a, v, c, min(E, a.cols - c), acc);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ very few lookups: the whole backward in one launch
+
+// The sort of embed_sort_few with the block's positions left in LDS, then the block sums (or clears) its rows at once.  Lane groups
+// take a row each; rows of more than kFusedLong lookups are shared out over all the groups and joined in LDS.
+constexpr int kFusedRows = 2048, kFusedLong = 32, kFusedUnroll = 8;
+constexpr int64_t kFusedNnz = 4096, kFusedWork = 1 << 23;
+template <int E> constexpr int fused_lds(int range) {
+  return range * kSortWaves * 2 + (int)kFusedNnz * 2 + (int)kFusedNnz / kFusedLong * 2 + kSortBlock * E * 4;
+}
+template <int GD, bool Whole, bool Add>
+__global__ __launch_bounds__(kSortBlock) void embed_bwd_few(const int32_t* __restrict__ ids, int n, int range,
+                                                            unsigned long long* __restrict__ first_bad, const Sums a) {
+  constexpr int E = dmt::ChunkElems<GD>::value, GB = dmt::EltBytes<GD>::value;
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  __shared__ uint32_t s_many;
+  uint16_t* list = (uint16_t*)(lds + range / 2 * kSortWaves);           // [kFusedNnz] positions in order of their rows
+  uint16_t* many = list + kFusedNnz;                                    // rows of many lookups
+  float* sums = (float*)(many + kFusedNnz / kFusedLong);
+  if (threadIdx.x == 0) s_many = 0;
+  const uint32_t rows = (uint32_t)a.rows, first = blockIdx.x * (uint32_t)range;
+  order_few(ids, n, rows, range, lds, first_bad, [&](uint32_t, uint32_t, uint32_t) {},
+            [&](uint32_t, uint32_t place, uint32_t, uint32_t at) { list[place] = (uint16_t)at; });
+  __syncthreads();
+  const uint16_t* ends = (const uint16_t*)lds + (kSortWaves - 1) * range;
+  const int lane = threadIdx.x & ((1 << a.log2_lpr) - 1), group = threadIdx.x >> a.log2_lpr;
+  const int groups = kSortBlock >> a.log2_lpr;
+  auto sum = [&](int from, int to, int c, int valid, float (&acc)[E]) {
+    for (int i = from; i < to; i += kFusedUnroll) {
+      dmt::Raw<GD, E> g[kFusedUnroll];
+#pragma unroll
+      for (int u = 0; u < kFusedUnroll; ++u)
+        if (i + u < to) g[u] = dmt::load_raw<GD, E>(a.grad + ((int64_t)list[i + u] * a.grad_stride + c) * GB, valid);
+#pragma unroll
+      for (int u = 0; u < kFusedUnroll; ++u) {
+        if (i + u >= to) break;
+        float x[E];
+        dmt::unpack<GD, E>(g[u], x);
+#pragma unroll
+        for (int q = 0; q < E; ++q) acc[q] += x[q];
+      }
+    }
+  };
+  for (int r = group; r < range && first + r < rows; r += groups) {
+    const int from = r > 0 ? ends[r - 1] : 0, to = ends[r];
+    if (to - from > kFusedLong) {
+      if (lane == 0) many[atomicAdd(&s_many, 1u)] = (uint16_t)r;        // (their order changes no sum)
+      continue;
+    }
+    if (Add && to == from) continue;
+    for (int c = lane * E; c < a.cols; c += E << a.log2_lpr) {
+      float acc[E];
+#pragma unroll
+      for (int q = 0; q < E; ++q) acc[q] = 0.f;
+      const int valid = Whole ? E : min(E, a.cols - c);
+      if (to == from) {
+        dmt::store_elems<DMT_F32, E>((char*)(a.out + (first + r) * a.out_stride + c), valid, acc);
+        continue;
+      }
+      sum(from, to, c, valid, acc);
+      write_row<E, Add>(a, first + r, c, valid, acc);
+    }
+  }
+  __syncthreads();
+  const int count = (int)s_many;
+  for (int i = 0; i < count; ++i) {
+    const int r = many[i], from = r > 0 ? ends[r - 1] : 0, to = ends[r];
+    const int per = (to - from + groups - 1) / groups, mine = min(to, from + group * per), end = min(to, mine + per);
+    for (int c0 = 0; c0 < a.cols; c0 += E << a.log2_lpr) {
+      const int c = c0 + lane * E, valid = Whole ? E : min(E, a.cols - c);
+      float acc[E];
+#pragma unroll
+      for (int q = 0; q < E; ++q) acc[q] = 0.f;
+      if (c < a.cols) sum(mine, end, c, valid, acc);
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < E; ++q) sums[threadIdx.x * E + q] = acc[q];
+      __syncthreads();
+      if (group == 0 && c < a.cols) {
+        for (int g = 1; g < groups; ++g)
+#pragma unroll
+          for (int q = 0; q < E; ++q) acc[q] += sums[((g << a.log2_lpr) + lane) * E + q];
+        write_row<E, Add>(a, first + r, c, valid, acc);
       }
     }
   }
@@ -476,18 +653,19 @@ struct Ws {
   uint8_t* touched;
   float* part;
   int64_t nblk, touched_words, ntiles;
-  bool few;                                  // one launch sorts
+  bool fused, few;                           // one launch does everything, sorts
   int range;                                 // rows of a block of it
   int items, passes, bits;
   int tile, part_cols;
   size_t bytes;
 };
 
-// Records a lane group walks: as many as leave a wave's worth of groups for every place on the chip, at least 8.
-constexpr int64_t kFillLanes = 256 * 2048;
-constexpr int kLeastTile = 8;
+// Records a lane group walks: as many as leave a wave's worth of groups for every place on the chip, at least kLeastTile (of 8: as fast,
+// and the join 45 us for 31).
+constexpr int64_t kFillLanes = 256 * 512;
+constexpr int kLeastTile = 16, kMostTile = 32;
 int tile_of(int64_t n, int64_t cols) {
-  int tile = 64;
+  int tile = kMostTile;
   const int lanes = 1 << log2_lanes(cols, 8);
   while (tile > kLeastTile && (n + tile - 1) / tile * lanes < kFillLanes) tile /= 2;
   return tile;
@@ -500,6 +678,9 @@ Ws carve(int64_t n, int64_t rows, int64_t cols, void* at) {
   int64_t blocks = std::max<int64_t>(kFewBlocks, (rows + kFewRows) / kFewRows);
   w.range = (int)dmt_align_up((size_t)((rows + blocks) / blocks), 32);   // the key `rows` included
   w.few = n <= kFewNnz && n * blocks <= kFewWork;
+  const int64_t narrow = std::max<int64_t>(kFewBlocks, (rows + kFusedRows - 1) / kFusedRows);
+  w.fused = n <= kFusedNnz && n * narrow <= kFusedWork;
+  if (w.fused) w.range = (int)dmt_align_up((size_t)((rows + narrow - 1) / narrow), 32);
   int bits = 1;
   while ((rows >> bits) != 0) ++bits;                    // the key `rows` included
   w.passes = (bits + kMaxDigit - 1) / kMaxDigit;
@@ -519,7 +700,7 @@ Ws carve(int64_t n, int64_t rows, int64_t cols, void* at) {
   // (never less for fewer lookups in smaller blocks and tiles: a workspace sized for the most serves all calls)
   const int64_t most_blk = std::max(w.nblk, std::min(kSortFill, (n + kSortBlock - 1) / kSortBlock));
   const int64_t most_tiles =
-      std::max((n + 63) / 64, std::min((n + kLeastTile - 1) / kLeastTile, 2 * kFillLanes >> log2_lanes(cols, 8)));
+      std::max((n + kMostTile - 1) / kMostTile, std::min((n + kLeastTile - 1) / kLeastTile, 2 * kFillLanes >> log2_lanes(cols, 8)));
   w.counts = (uint32_t*)take(sizeof(uint32_t) * ((size_t)most_blk << w.bits));
   w.totals = (uint32_t*)take(sizeof(uint32_t) << w.bits);
   w.touched = (uint8_t*)take(sizeof(uint32_t) * (size_t)w.touched_words);
@@ -547,13 +728,40 @@ void launch_fwd(int32_t od, const void* table, int64_t rows, int64_t cols, int64
   else go(embed_fwd_kernel<TD, DMT_BF16>);
 }
 
+// The sums' share of the clearing, percent; the join has the rest.  (With a tenth in each of the sort's last launches too
+// the whole call took as long: what they hide they cost.)
+constexpr int kSumsShare = 55;
+
+// The table's rows in wave units, handed out to the two launches.
+struct Clearing {
+  Fill fill = {};
+  int64_t units = 0, done = 0;
+  Clearing(const Ws& w, const Sums& a) {
+    fill.touched = w.touched, fill.out = a.out, fill.out_stride = a.out_stride, fill.rows = a.rows, fill.cols = a.cols;
+    fill.log2_lanes = log2_lanes(a.cols, 4);
+    const int64_t per = std::min<int64_t>(64, std::min(kFillBytes / (4 * (int64_t)a.cols), a.rows / kFillWaves));
+    fill.rows_per_wave = (int)std::max<int64_t>(64 >> fill.log2_lanes, per);
+    if (!a.accumulate) units = (a.rows + fill.rows_per_wave - 1) / fill.rows_per_wave;
+  }
+  // A launch of `own` blocks of `waves` waves takes `percent` of all the units: its grid, with `f` for its kernel.
+  dim3 share(unsigned own, int waves, int percent, Fill& f) {
+    f = fill;
+    f.own_blocks = own;
+    f.first = done;
+    const int64_t want = percent >= 100 ? units - done : std::min(units - done, units * percent / 100);
+    const int64_t blocks = (want + waves - 1) / waves;
+    done = std::min(units, done + blocks * waves);
+    return dim3((unsigned)(own + blocks));
+  }
+};
+
 template <bool First>
 void launch_pass(const Ws& w, const int32_t* ids, const uint64_t* in, uint64_t* out, int64_t n, int64_t rows,
                  int shift, int64_t* bad, hipStream_t s) {
   const int nd = 1 << w.bits;
   hipLaunchKernelGGL(embed_digits<First>, dim3((unsigned)w.nblk), dim3(kSortBlock), 0, s, ids, in, n, (uint32_t)rows,
                      w.items, shift, w.bits, w.counts, (uint32_t*)w.touched, w.touched_words, (unsigned long long*)bad);
-  hipLaunchKernelGGL(embed_digit_starts, dim3((nd + 63) / 64), dim3(64), 0, s, w.counts, w.nblk, nd, w.totals);
+  hipLaunchKernelGGL(embed_digit_starts, dim3((nd + 63) / 64), dim3(64 * kStartsSegs), 0, s, w.counts, w.nblk, nd, w.totals);
   static DmtPerDevice done;
   dmt_allow_lds(done, (const void*)embed_scatter<First>, (4 + 2 * kSortWaves) << kMaxDigit);
   hipLaunchKernelGGL(embed_scatter<First>, dim3((unsigned)w.nblk), dim3(kSortBlock), (4 + 2 * kSortWaves) << w.bits, s,
@@ -568,19 +776,42 @@ void launch_few(const Ws& w, const int32_t* ids, int64_t n, int64_t rows, int64_
                      (unsigned long long*)bad);
 }
 
+// run(whole pieces, add to what is there), each a std::true_type or std::false_type.
+template <typename Run> void variants(bool whole, bool add, Run run) {
+  if (whole) add ? run(std::true_type(), std::true_type()) : run(std::true_type(), std::false_type());
+  else add ? run(std::false_type(), std::true_type()) : run(std::false_type(), std::false_type());
+}
+
 template <int GD>
-void launch_sums(Sums a, hipStream_t s) {
-  a.log2_lpr = log2_lanes(a.cols, dmt::ChunkElems<GD>::value);
-  a.slices = (a.cols + (dmt::ChunkElems<GD>::value << a.log2_lpr) - 1) / (dmt::ChunkElems<GD>::value << a.log2_lpr);
+void launch_fused(const Ws& w, Sums a, const int32_t* ids, int64_t* bad, hipStream_t s) {
+  constexpr int E = dmt::ChunkElems<GD>::value;
+  a.log2_lpr = log2_lanes(a.cols, E);
+  variants(a.cols % E == 0, a.accumulate, [&](auto whole, auto add) {
+    auto kernel = embed_bwd_few<GD, decltype(whole)::value, decltype(add)::value>;
+    static DmtPerDevice done;
+    dmt_allow_lds(done, (const void*)kernel, fused_lds<E>(kFusedRows));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.rows + w.range - 1) / w.range)), dim3(kSortBlock), fused_lds<E>(w.range), s,
+                       ids, (int)a.n, w.range, (unsigned long long*)bad, a);
+  });
+}
+
+template <int GD>
+void launch_sums(Sums a, Clearing& clear, hipStream_t s) {
+  constexpr int E = dmt::ChunkElems<GD>::value;
+  a.log2_lpr = log2_lanes(a.cols, E);
+  a.log2_join = log2_lanes(a.cols, 4);
+  a.slices = (a.cols + (E << a.log2_lpr) - 1) / (E << a.log2_lpr);
   const int groups = kBlock >> a.log2_lpr;
-  a.tile_blocks = (a.ntiles + groups - 1) / groups * a.slices;
-  a.log2_fill = log2_lanes(a.cols, 4);
-  a.fill_rows = (int)std::max<int64_t>(kBlock >> a.log2_fill, kFillBytes / (4 * a.cols));
-  const int64_t fill_blocks = a.accumulate ? 0 : (a.rows + a.fill_rows - 1) / a.fill_rows;
-  if (a.tile_blocks + fill_blocks > 0)
-    hipLaunchKernelGGL(embed_sums<GD>, dim3((unsigned)(a.tile_blocks + fill_blocks)), dim3(kBlock), 0, s, a);
-  if (a.ntiles > 1)
-    hipLaunchKernelGGL(embed_join, dim3((unsigned)((a.ntiles + kJoinTiles - 1) / kJoinTiles)), dim3(kBlock), 0, s, a);
+  const bool join = a.ntiles > 1;                           // (else no run is long)
+  const dim3 sums = clear.share((unsigned)((a.ntiles + groups - 1) / groups * a.slices), kBlock / 64, join ? kSumsShare : 100, a.fill);
+  if (sums.x > 0)
+    variants(a.cols % E == 0, a.accumulate, [&](auto whole, auto add) {
+      hipLaunchKernelGGL((embed_sums<GD, decltype(whole)::value, decltype(add)::value>), sums, dim3(kBlock), 0, s, a);
+    });
+  if (!join) return;
+  const dim3 grid = clear.share((unsigned)((a.ntiles + kJoinTiles - 1) / kJoinTiles), kJoinBlock / 64, 100, a.fill);
+  if (a.accumulate) hipLaunchKernelGGL(embed_join<true>, grid, dim3(kJoinBlock), 0, s, a);
+  else hipLaunchKernelGGL(embed_join<false>, grid, dim3(kJoinBlock), 0, s, a);
 }
 
 }  // namespace
@@ -625,6 +856,17 @@ extern "C" dmt_status dmt_embed_bwd(const int32_t* ids, int64_t n, const void* g
   const Ws w = carve(n, rows, cols, workspace);
   if (workspace_bytes < w.bytes) return DMT_ENOMEM;
   hipStream_t s = (hipStream_t)stream;
+  Sums a = {};
+  a.n = n, a.rows = rows, a.grad = (const char*)grad, a.grad_stride = grad_stride, a.scale = scale;
+  a.out = grad_table, a.out_stride = grad_table_stride, a.cols = (int)cols, a.accumulate = accumulate != 0;
+  a.tile = w.tile, a.ntiles = w.ntiles, a.part = w.part, a.part_cols = w.part_cols;
+  if (w.fused) {
+    if (grad_dtype == DMT_F32) launch_fused<DMT_F32>(w, a, ids, first_bad, s);
+    else if (grad_dtype == DMT_F16) launch_fused<DMT_F16>(w, a, ids, first_bad, s);
+    else launch_fused<DMT_BF16>(w, a, ids, first_bad, s);
+    return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
+  }
+  Clearing clear(w, a);
   uint64_t *in = w.b, *out = w.a;
   if (w.few) {
     launch_few(w, ids, n, rows, first_bad, s);
@@ -635,13 +877,9 @@ extern "C" dmt_status dmt_embed_bwd(const int32_t* ids, int64_t n, const void* g
     else launch_pass<false>(w, ids, in, out, n, rows, p * w.bits, first_bad, s);
     std::swap(in, out);
   }
-  Sums a = {};
-  a.recs = in, a.n = n, a.rows = rows;
-  a.grad = (const char*)grad, a.grad_stride = grad_stride, a.scale = scale;
-  a.out = grad_table, a.out_stride = grad_table_stride, a.cols = (int)cols, a.accumulate = accumulate != 0;
-  a.tile = w.tile, a.ntiles = w.ntiles, a.part = w.part, a.part_cols = w.part_cols, a.touched = w.touched;
-  if (grad_dtype == DMT_F32) launch_sums<DMT_F32>(a, s);
-  else if (grad_dtype == DMT_F16) launch_sums<DMT_F16>(a, s);
-  else launch_sums<DMT_BF16>(a, s);
+  a.recs = in;
+  if (grad_dtype == DMT_F32) launch_sums<DMT_F32>(a, clear, s);
+  else if (grad_dtype == DMT_F16) launch_sums<DMT_F16>(a, clear, s);
+  else launch_sums<DMT_BF16>(a, clear, s);
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }

@@ -118,7 +118,9 @@ def test_embed_fwd(dmt, n, rows, cols, pad, shift, td, od):
 
 @pytest.mark.parametrize("kind", ["uniform", "skew", "one", "sorted", "holes", "none"])
 @pytest.mark.parametrize("gd", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("n,rows,cols,pad,shift", SHAPES + [(0, 5, 7, 0, 0), (6000, 300, 24, 0, 0), (9000, 3000, 16, 1, 0)])
+@pytest.mark.parametrize("n,rows,cols,pad,shift", SHAPES + [(0, 5, 7, 0, 0), (4096, 300, 24, 0, 0), (4097, 300, 24, 0, 0),
+                                                          (9000, 3000, 16, 1, 0), (4500, 3, 5, 1, 1),
+                                                          (4200, 40, 1030, 2, 3), (5000, 333, 130, 0, 0), (66_000, 70, 40, 3, 1)])
 def test_embed_bwd(dmt, n, rows, cols, pad, shift, gd, kind):
     rng = np.random.default_rng(n + 3 * cols)
     ids = some_ids(rng, n, rows, kind)
