@@ -563,13 +563,15 @@ dmt_status dmt_layer_norm_bwd(const void* x, int64_t rows, int64_t cols, int64_t
  *   stats[r]    = { max_j x_j, sum_j exp(x_j - max) }, what the backward reads
  * A score of -inf is masked: it takes no part in anything (a masked target has logprob -inf).  A row
  * whose mask leaves nothing has logprob -inf (0 without a target), entropy 0, no top items, stats {-inf, 0} and no gradient.
- * A row that holds a NaN or +inf has NaN for logprob and entropy; its top items are some items of
- * the row, or -1.  Scores at the type's lowest finite value are ordinary scores.
+ * A row that holds a NaN or +inf has NaN for logprob (0 without a target) and entropy; its top items
+ * are some items of the row, or -1.  Scores at the type's lowest finite value are ordinary scores.
  *   x        [rows][vocab] of dtype;  targets dev int32 [rows], NULL when logprob is
  *   logprob, entropy  float32 [rows];  stats float32 [rows][2];  top_ids int32 [rows][k],
  *            top_logprobs float32 [rows][k];  any of them may be NULL (top_logprobs needs top_ids)
  *   k        0 ... DMT_TOP_MAX (0: no top items; may exceed vocab)
- * vocab >= 1, rows >= 0; DMT_ENOTSUP for rows beyond 2^31 - 1 or vocab beyond 2^30.
+ *   workspace of the size for (rows, vocab, k); one sized for more rows serves fewer
+ * vocab >= 1, rows >= 0; DMT_ENOTSUP for rows beyond 2^31 - 1, vocab beyond 2^30 or more than 2^31 - 1
+ * pieces of 4096 scores in all.
  */
 #define DMT_TOP_MAX 64
 size_t dmt_token_logprob_workspace_bytes(int64_t rows, int64_t vocab, int32_t k);

@@ -1,6 +1,14 @@
 // dmt_token_logprob_fwd, dmt_token_logprob_bwd: rows of scores as distributions.
 //   M = max x, S = sum exp(x - M), T = sum exp(x - M) (x - M):  log p_j = x_j - M - log S,  H = log S - T / S.
+//
+// Forward, one pass over the scores.  A block takes a span of a row, 16 KB at a time in registers; every lane keeps a maximum, S
+// and T of its own and rescales them when its maximum grows.  Exponents are kept to the base 2: z = x log2 e - M log2 e is one
+// fused multiply-add, and M's product is rounded once and the same in every term (and in the backward), so its error cancels.
+// The top k: each wave holds its 64 best so far, sorted, one a lane.  The k-th largest of the lanes' maxima of a piece is a
+// bound that at least k scores reach, so only the few scores above it (and above the list's k-th) are looked at singly.
+// Rows are cut into spans when they are too few to fill the chip; a second launch joins the spans.
 #include <algorithm>
+#include <type_traits>
 
 #include "dmt_internal.h"
 #include "dmt_rows.h"
@@ -8,108 +16,370 @@
 namespace {
 
 constexpr int kBlock = 256, kWaves = kBlock / 64;
+constexpr int kVecs = 4;                                   // 16-byte pieces of a lane under way
 constexpr float kInf = __builtin_inff();
+constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
+constexpr float kFar = 1e30f;                              // |M| beyond which M log2 e may overflow
+constexpr float kNone = -200.f;                            // 2^kNone is 0: stands for exponents down to -inf
 
-template <int DT>
-__global__ __launch_bounds__(kBlock) void logprob_fwd(const char* __restrict__ x, int vocab, int64_t stride,
-                                                      const int32_t* __restrict__ targets,
-                                                      float* __restrict__ logprob, float* __restrict__ entropy,
-                                                      float* __restrict__ stats, int k,
-                                                      int32_t* __restrict__ top_ids,
-                                                      float* __restrict__ top_logprobs,
-                                                      unsigned long long* __restrict__ first_bad) {
-  constexpr int EB = dmt::EltBytes<DT>::value;
-  __shared__ float sm[kWaves];
-  __shared__ int si[kWaves];
-  const int64_t r = blockIdx.x;
-  const char* xr = x + r * stride * EB;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float m = -kInf;
-  for (int j = threadIdx.x; j < vocab; j += kBlock) m = fmaxf(m, dmt::load1<DT>(xr + (int64_t)j * EB));
-  m = dmt::group_max<64>(m);
-  if (lane == 0) sm[wave] = m;
-  __syncthreads();
-  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, sm[w]);
-  __syncthreads();
-  float s = 0.f, t = 0.f;
-  for (int j = threadIdx.x; j < vocab; j += kBlock) {
-    const float v = dmt::load1<DT>(xr + (int64_t)j * EB);
-    if (v == -kInf) continue;
-    const float z = v - m, e = __expf(z);
-    s += e;
-    t += e * z;
-  }
-  s = dmt::block_sum<kWaves>(s, sm);
-  t = dmt::block_sum<kWaves>(t, sm);
-  const bool empty = s == 0.f;
-  const float ls = logf(s);
-  if (threadIdx.x == 0) {
-    const int32_t at = targets ? targets[r] : -1;
-    if (at >= vocab && first_bad) atomicMin(first_bad, (unsigned long long)r);
-    if (logprob)
-      logprob[r] = at < 0 || at >= vocab ? 0.f : empty ? -kInf : dmt::load1<DT>(xr + (int64_t)at * EB) - m - ls;
-    if (entropy) entropy[r] = empty ? 0.f : ls - t / s;
-    if (stats) stats[2 * r] = m, stats[2 * r + 1] = s;
-  }
-  // the largest score behind the last one taken, k times over
-  float last = kInf;
-  int last_at = -1;
-  for (int i = 0; i < k; ++i) {
-    float best = -kInf;
-    int at = -1;
-    if (last != -kInf)
-      for (int j = threadIdx.x; j < vocab; j += kBlock) {
-        const float v = dmt::load1<DT>(xr + (int64_t)j * EB);
-        if ((v < last || (v == last && j > last_at)) && v > best) best = v, at = j;
-      }
+template <int DT> constexpr int piece_elems() { return kBlock * kVecs * dmt::ChunkElems<DT>::value; }
+
+// (x - m) log2 e;  m is not -inf.
+__device__ __forceinline__ float exponent(float x, float m) {
+  return fabsf(m) > kFar ? (x - m) * kLog2e : fmaf(x, kLog2e, -(m * kLog2e));
+}
+__device__ __forceinline__ float or_zero(float m) { return m == -kInf ? 0.f : m; }
+
+// log p of score x;  ls = log2 S.  (Far below M, exponents of 2 would overflow before natural ones do.)
+__device__ __forceinline__ float log_prob(float x, float m, float ls) {
+  return fabsf(x - m) > kFar ? x - m - ls * kLn2 : (exponent(x, m) - ls) * kLn2;
+}
+
+struct Sum {
+  float m, s, t;                                           // t in units of ln 2
+};
+
+// What `a` is with the maximum m (>= a.m).  Its terms hold a.m's rounded product, so that is what is taken back: equal
+// maxima leave the sums as they are.
+__device__ __forceinline__ void rescale(Sum& a, float m) {
+#pragma clang fp contract(off)
+  const float far = (a.m - m) * kLog2e, near = a.m * kLog2e - m * kLog2e;
+  const float d = a.m == -kInf ? kNone : fabsf(m) > kFar ? far : near, f = __builtin_amdgcn_exp2f(d);
+  a.t = f == 0.f ? 0.f : f * fmaf(d, a.s, a.t);
+  a.s *= f;                                                // (a NaN stays)
+  a.m = m;
+}
+
+// ------------------------------------------------------------------ sorted lists, one entry a lane
+
+// An entry orders by score, then by the lower item: larger entries are better, 0 is none.
+__device__ __forceinline__ uint64_t entry(float v, uint32_t item) {
+  const uint32_t u = __float_as_uint(v == 0.f ? 0.f : v);  // (zeros of both signs tie)
+  return (uint64_t)((u >> 31) ? ~u : u | 0x80000000u) << 32 | (0xffffffffu - item);
+}
+__device__ __forceinline__ float entry_score(uint64_t e) {
+  const uint32_t u = (uint32_t)(e >> 32);
+  return e == 0 ? -kInf : __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ uint32_t entry_item(uint64_t e) { return 0xffffffffu - (uint32_t)e; }
+
+template <typename V> __device__ __forceinline__ V larger(V a, V b) { return a > b ? a : b; }
+template <typename V> __device__ __forceinline__ V smaller(V a, V b) { return a > b ? b : a; }
+
+// A sequence that rises, then falls (or the other way round) into falling order.
+template <typename V> __device__ __forceinline__ V merge_falling(V v) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const float b = __shfl_xor(best, o);
-      const int a = __shfl_xor(at, o);
-      if (b > best || (b == best && a >= 0 && a < at)) best = b, at = a;
+  for (int o = 32; o > 0; o >>= 1) {
+    const V w = __shfl_xor(v, o);
+    v = lane & o ? smaller(v, w) : larger(v, w);
+  }
+  return v;
+}
+template <typename V, bool Falling> __device__ __forceinline__ V sort64(V v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int n = 2; n <= 64; n *= 2)
+#pragma unroll
+    for (int o = n / 2; o > 0; o >>= 1) {
+      const V w = __shfl_xor(v, o);
+      const bool low = (lane & o) == 0, falling = ((lane & n) == 0) == Falling;
+      v = low == falling ? larger(v, w) : smaller(v, w);
     }
-    if (lane == 0) sm[wave] = best, si[wave] = at;
-    __syncthreads();
-    best = -kInf, at = -1;
-    for (int w = 0; w < kWaves; ++w)
-      if (sm[w] > best || (sm[w] == best && si[w] >= 0 && si[w] < at)) best = sm[w], at = si[w];
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      top_ids[r * k + i] = at;
-      if (top_logprobs) top_logprobs[r * k + i] = at < 0 ? -kInf : best - m - ls;
-    }
-    last = best, last_at = at;
+  return v;
+}
+// The 64 best of a falling list and of 64 entries in any order.
+__device__ __forceinline__ uint64_t add64(uint64_t list, uint64_t more) {
+  return merge_falling(larger(list, sort64<uint64_t, false>(more)));
+}
+
+// The waves' lists into one, in wave 0.  lds [kWaves][64].
+__device__ __forceinline__ uint64_t join_lists(uint64_t list, uint64_t (*lds)[64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  lds[wave][lane] = list;
+  __syncthreads();
+  if (wave == 0)
+    for (int w = 1; w < kWaves; ++w) list = merge_falling(larger(list, lds[w][63 - lane]));
+  return list;
+}
+
+// The threads' sums into one, the same in every thread.  Ends with a barrier.
+__device__ __forceinline__ Sum join_sums(Sum a, float (*lds)[3]) {
+  rescale(a, dmt::group_max<64>(a.m));
+  a.s = dmt::group_sum<64>(a.s);
+  a.t = dmt::group_sum<64>(a.t);
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) lds[wave][0] = a.m, lds[wave][1] = a.s, lds[wave][2] = a.t;
+  __syncthreads();
+  Sum all = {-kInf, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) all.m = fmaxf(all.m, lds[w][0]);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    Sum b = {lds[w][0], lds[w][1], lds[w][2]};
+    rescale(b, all.m);
+    all.s += b.s;
+    all.t += b.t;
+  }
+  __syncthreads();
+  return all;
+}
+
+// ------------------------------------------------------------------ forward
+
+struct Fwd {
+  const char* x;
+  int64_t stride;
+  int vocab, k, spans, span;                               // span: elements, a multiple of the piece
+  const int32_t* targets;
+  float *logprob, *entropy, *stats;
+  int32_t* top_ids;
+  float* top_logprobs;
+  unsigned long long* first_bad;
+  float4* part;                                            // [row][span] sums
+  uint64_t* lists;                                         // [row][span][k]
+};
+
+// A row's answers from its sums (known to every thread) and its list (wave 0's).
+template <int DT>
+__device__ __forceinline__ void finish(const Fwd& a, int64_t row, const Sum& all, uint64_t list) {
+  constexpr int EB = dmt::EltBytes<DT>::value;
+  const bool empty = all.s == 0.f;
+  const float m = or_zero(all.m), ls = log2f(all.s);
+  if (threadIdx.x == 0) {
+    const int32_t at = a.targets ? a.targets[row] : -1;
+    if (at >= a.vocab && a.first_bad) atomicMin(a.first_bad, (unsigned long long)row);
+    if (a.logprob)
+      a.logprob[row] = at < 0 || at >= a.vocab ? 0.f
+                       : empty                 ? -kInf
+                                               : log_prob(dmt::load1<DT>(a.x + (row * a.stride + at) * EB), m, ls);
+    if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - all.t / all.s) * kLn2;
+    if (a.stats) a.stats[2 * row] = all.m, a.stats[2 * row + 1] = all.s;
+  }
+  if ((int)threadIdx.x < a.k) {
+    a.top_ids[row * a.k + threadIdx.x] = list ? (int32_t)entry_item(list) : -1;
+    if (a.top_logprobs) a.top_logprobs[row * a.k + threadIdx.x] = list ? log_prob(entry_score(list), m, ls) : -kInf;
   }
 }
 
+// 16 KB of a row from element j on, -inf behind `end`.
 template <int DT>
-__global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, int64_t stride,
+__device__ __forceinline__ void load_piece(const char* row, int j, int end, dmt::Raw<DT, dmt::ChunkElems<DT>::value> (&r)[kVecs]) {
+  constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value, W = dmt::Raw<DT, E>::kWords;
+  constexpr uint32_t kMasked = DT == DMT_F32 ? 0xff800000u : DT == DMT_F16 ? 0xfc00fc00u : 0xff80ff80u;
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) {
+    const int at = j + (v * kBlock + (int)threadIdx.x) * E, valid = end - at;
+    if (valid > 0) r[v] = dmt::load_raw<DT, E>(row + (int64_t)at * EB, valid);
+    if (valid < E) {
+#pragma unroll
+      for (int q = 0; q < W; ++q) {
+        if constexpr (DT == DMT_F32) {
+          if (q >= valid) r[v].w[q] = kMasked;
+        } else {
+          if (q * 2 >= valid) r[v].w[q] = kMasked;
+          else if (q * 2 + 1 >= valid) r[v].w[q] = (r[v].w[q] & 0xffffu) | (kMasked & 0xffff0000u);
+        }
+      }
+    }
+  }
+}
+
+template <int DT, bool Top>
+__global__ __launch_bounds__(kBlock) void logprob_spans(const Fwd a) {
+  constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
+  __shared__ float s_sum[kWaves][3];
+  __shared__ uint64_t s_list[kWaves][128];                 // candidates of each wave; its list at the end
+  const int64_t row = blockIdx.x / (unsigned)a.spans;
+  const int span = (int)(blockIdx.x % (unsigned)a.spans);
+  const char* x = a.x + row * a.stride * EB;
+  const int begin = span * a.span, end = min(a.vocab, begin + a.span);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Sum sum = {-kInf, 0.f, 0.f};
+  uint64_t list = 0;
+  float cut = -kInf;                                       // scores up to it are not among the k best
+  int waiting = 0;
+  uint64_t* buf = s_list[wave];
+  // takes up to 64 of the waiting candidates into the list
+  auto take = [&]() {
+    const int from = max(0, waiting - 64);
+    const uint64_t e = from + lane < waiting ? buf[from + lane] : 0;
+    __builtin_amdgcn_wave_barrier();
+    waiting = from;
+    list = add64(list, e);
+  };
+  dmt::Raw<DT, E> r[kVecs], next[kVecs];
+  load_piece<DT>(x, begin, end, next);
+  for (int j = begin; j < end; j += piece_elems<DT>()) {
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) r[v] = next[v];
+    if (j + piece_elems<DT>() < end) load_piece<DT>(x, j + piece_elems<DT>(), end, next);
+    float most[kVecs], pm = -kInf;
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+      float e[E];
+      dmt::unpack<DT, E>(r[v], e);
+      most[v] = e[0];
+#pragma unroll
+      for (int q = 1; q < E; ++q) most[v] = fmaxf(most[v], e[q]);
+      pm = fmaxf(pm, most[v]);
+    }
+    if (pm > sum.m) rescale(sum, pm);
+    const float m = or_zero(sum.m), m2 = m * kLog2e;
+    auto add = [&](auto z) {
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) {
+        float e[E];
+        dmt::unpack<DT, E>(r[v], e);
+#pragma unroll
+        for (int q = 0; q < E; ++q) {
+          const float d = z(e[q]), p = __builtin_amdgcn_exp2f(d);
+          sum.s += p;
+          sum.t = fmaf(p, fmaxf(d, kNone), sum.t);
+        }
+      }
+    };
+    if (__any(fabsf(m) > kFar)) add([&](float v) { return exponent(v, m); });
+    else add([&](float v) { return fmaf(v, kLog2e, -m2); });
+    if constexpr (Top) {
+      const uint64_t over = __ballot(pm > cut);
+      if (over) {
+        float low = cut;                                   // of this piece, candidates are above it
+        if (__popcll(over) >= a.k) {
+          // at least k scores reach the k-th largest of the lanes' maxima; equal ones may have lower items
+          const float bound = __shfl(sort64<float, true>(pm), a.k - 1);
+          const uint32_t u = __float_as_uint(bound);
+          const float below = bound == 0.f ? -__uint_as_float(1u) : __uint_as_float(bound > 0.f ? u - 1 : u + 1);
+          low = fmaxf(low, bound == -kInf ? bound : below);
+        }
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+          if (!__any(most[v] > low)) continue;
+          float e[E];
+          dmt::unpack<DT, E>(r[v], e);
+#pragma unroll
+          for (int q = 0; q < E; ++q) {
+            const uint64_t mask = __ballot(e[q] > low);
+            if (!mask) continue;
+            if (mask >> lane & 1)
+              buf[waiting + __popcll(mask & ((1ull << lane) - 1))] =
+                  entry(e[q], (uint32_t)(j + (v * kBlock + (int)threadIdx.x) * E + q));
+            __builtin_amdgcn_wave_barrier();
+            waiting += __popcll(mask);
+            if (waiting >= 64) take();
+          }
+        }
+        if (waiting > 0 && (j == begin || j + piece_elems<DT>() >= end)) take();
+        // later pieces hold later items only: a score has to beat the k-th
+        const float kth = __shfl(entry_score(list), a.k - 1);
+        cut = fmaxf(cut, kth);
+      }
+    }
+  }
+  if (Top && waiting > 0) take();
+  sum = join_sums(sum, s_sum);
+  if constexpr (Top) list = join_lists(list, (uint64_t(*)[64])s_list);
+  if (a.spans == 1) {
+    finish<DT>(a, row, sum, list);
+  } else {
+    const int64_t at = row * a.spans + span;
+    if (threadIdx.x == 0) a.part[at] = make_float4(sum.m, sum.s, sum.t, 0.f);
+    if (Top && (int)threadIdx.x < a.k) a.lists[at * a.k + threadIdx.x] = list;
+  }
+}
+
+// A row's spans into one.
+template <int DT, bool Top>
+__global__ __launch_bounds__(kBlock) void logprob_join(const Fwd a) {
+  __shared__ float s_sum[kWaves][3];
+  __shared__ uint64_t s_list[kWaves][64];
+  const int64_t row = blockIdx.x;
+  Sum sum = {-kInf, 0.f, 0.f};
+  for (int i = threadIdx.x; i < a.spans; i += kBlock) {
+    const float4 p = a.part[row * a.spans + i];
+    Sum b = {p.x, p.y, p.z};
+    const float m = fmaxf(sum.m, b.m);
+    rescale(sum, m);
+    rescale(b, m);
+    sum.s += b.s;
+    sum.t += b.t;
+  }
+  uint64_t list = 0;
+  if constexpr (Top) {
+    const int count = a.spans * a.k, lane = threadIdx.x & 63;
+    const uint64_t* from = a.lists + row * a.spans * a.k;
+    for (int i = (int)(threadIdx.x >> 6) * 64; i < count; i += kBlock) {
+      const uint64_t e = i + lane < count ? from[i + lane] : 0;
+      if (__any(e > __shfl(list, a.k - 1))) list = add64(list, e);
+    }
+    list = join_lists(list, s_list);
+  }
+  sum = join_sums(sum, s_sum);
+  finish<DT>(a, row, sum, list);
+}
+
+// ------------------------------------------------------------------ backward
+
+// dx = p (A + B z) with p = exp2(z) / S, z to the base 2:  A = -g_lp - g_H (H - log S),  B = -g_H ln 2.
+template <int DT>
+__global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, int64_t stride, int pieces,
                                                       const int32_t* __restrict__ targets,
                                                       const float* __restrict__ stats,
                                                       const float* __restrict__ entropy,
                                                       const float* __restrict__ grad_logprob,
                                                       const float* __restrict__ grad_entropy, char* dx,
                                                       int64_t dx_stride) {
-  constexpr int EB = dmt::EltBytes<DT>::value;
-  const int64_t r = blockIdx.x;
-  const char* xr = x + r * stride * EB;
-  char* dr = dx + r * dx_stride * EB;
-  const float m = stats[2 * r], s = stats[2 * r + 1];
-  const int32_t at = targets ? targets[r] : -1;
-  const bool aimed = at >= 0 && at < vocab;
-  const float gl = grad_logprob && aimed ? grad_logprob[r] : 0.f;
-  const float gh = grad_entropy ? grad_entropy[r] : 0.f, h = grad_entropy ? entropy[r] : 0.f;
-  const float inv = 1.f / s, ls = logf(s);
-  for (int j = threadIdx.x; j < vocab; j += kBlock) {
-    const float v = dmt::load1<DT>(xr + (int64_t)j * EB);
-    float d = 0.f;
-    if (v != -kInf) {
-      const float z = v - m, p = __expf(z) * inv;
-      d = -gl * p - gh * (p * (z - ls + h));
-      if (j == at) d += gl;
+  constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
+  const int64_t row = blockIdx.x / (unsigned)pieces;
+  const int j = (int)(blockIdx.x % (unsigned)pieces) * piece_elems<DT>();
+  const char* xr = x + row * stride * EB;
+  char* dr = dx + row * dx_stride * EB;
+  dmt::Raw<DT, E> r[kVecs];
+  load_piece<DT>(xr, j, vocab, r);
+  const float m = or_zero(stats[2 * row]), s = stats[2 * row + 1], inv = s == 0.f ? 0.f : 1.f / s;
+  const int32_t at = targets ? targets[row] : -1;
+  const float gl = grad_logprob && at >= 0 && at < vocab ? grad_logprob[row] : 0.f;
+  const float gh = grad_entropy ? grad_entropy[row] : 0.f, h = grad_entropy ? entropy[row] : 0.f;
+  const float A = s == 0.f ? 0.f : (-gl - gh * (h - logf(s))) * inv, B = -gh * kLn2 * inv, m2 = m * kLog2e;
+  auto grads = [&](auto z) {
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+      const int c = j + (v * kBlock + (int)threadIdx.x) * E;
+      if (c >= vocab) break;
+      float e[E], d[E];
+      dmt::unpack<DT, E>(r[v], e);
+#pragma unroll
+      for (int q = 0; q < E; ++q) {
+        const float w = z(e[q]);
+        d[q] = __builtin_amdgcn_exp2f(w) * fmaf(B, fmaxf(w, kNone), A);
+      }
+      if (gl != 0.f && (uint32_t)(at - c) < (uint32_t)E) {
+#pragma unroll
+        for (int q = 0; q < E; ++q)
+          if (c + q == at && e[q] != -kInf) d[q] += gl;
+      }
+      dmt::store_elems<DT, E>(dr + (int64_t)c * EB, min(E, vocab - c), d);
     }
-    dmt::store1<DT>(dr + (int64_t)j * EB, d);
-  }
+  };
+  if (fabsf(m) > kFar) grads([&](float v) { return exponent(v, m); });
+  else grads([&](float v) { return fmaf(v, kLog2e, -m2); });
+}
+
+// A row is cut into spans of whole pieces while the blocks are fewer than fit the chip at once.
+struct Spans {
+  int spans, span;
+};
+constexpr int64_t kFillBlocks = 2048;
+Spans spans_of(int64_t rows, int64_t vocab, int64_t piece) {
+  const int64_t pieces = (vocab + piece - 1) / piece;
+  const int64_t want = std::min(pieces, std::max<int64_t>(1, (kFillBlocks + rows - 1) / std::max<int64_t>(rows, 1)));
+  const int64_t per = (pieces + want - 1) / want;
+  return {(int)((pieces + per - 1) / per), (int)(per * piece)};
+}
+
+// Sums and lists of so many spans.
+size_t part_bytes(int64_t spans, int k) {
+  return dmt_align_up(sizeof(float4) * (size_t)spans, 256) + sizeof(uint64_t) * (size_t)spans * (size_t)k;
 }
 
 bool fits(int64_t rows, int64_t vocab) { return rows < (1ll << 31) && vocab <= (1ll << 30); }
@@ -118,7 +388,9 @@ bool fits(int64_t rows, int64_t vocab) { return rows < (1ll << 31) && vocab <= (
 
 extern "C" size_t dmt_token_logprob_workspace_bytes(int64_t rows, int64_t vocab, int32_t k) {
   if (rows < 0 || vocab < 1 || k < 0 || k > DMT_TOP_MAX || !fits(rows, vocab)) return 0;
-  return 0;
+  // the most that any type, and any fewer rows, can need
+  const int64_t pieces = (vocab + piece_elems<DMT_F32>() - 1) / piece_elems<DMT_F32>();
+  return part_bytes(std::min(rows * pieces, kFillBlocks + rows), k);
 }
 
 extern "C" dmt_status dmt_token_logprob_fwd(const void* x, int64_t rows, int64_t vocab, int64_t x_stride,
@@ -132,18 +404,32 @@ extern "C" dmt_status dmt_token_logprob_fwd(const void* x, int64_t rows, int64_t
     return DMT_EINVAL;
   if (rows > 0 && (!dmt_is_at(x, dmt_ebytes(dtype)) || (logprob && !targets) || (k > 0 && !top_ids))) return DMT_EINVAL;
   if (!fits(rows, vocab)) return DMT_ENOTSUP;
-  const size_t need = dmt_token_logprob_workspace_bytes(rows, vocab, k);
-  if (need > 0 && !dmt_is_at(workspace, 256)) return DMT_EINVAL;
-  if (workspace_bytes < need) return DMT_ENOMEM;
+  const int64_t piece = dtype == DMT_F32 ? piece_elems<DMT_F32>() : piece_elems<DMT_BF16>();
+  const Spans sp = spans_of(rows, vocab, piece);
   if (rows == 0) return DMT_OK;
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kBlock), 0, (hipStream_t)stream, (const char*)x, (int)vocab,
-                       x_stride, targets, logprob, entropy, stats, (int)k, top_ids, top_logprobs,
-                       (unsigned long long*)first_bad);
+  if (rows * sp.spans >= (1ll << 31)) return DMT_ENOTSUP;
+  if (sp.spans > 1) {
+    if (!dmt_is_at(workspace, 256)) return DMT_EINVAL;
+    if (workspace_bytes < part_bytes(rows * sp.spans, k)) return DMT_ENOMEM;
+  }
+  Fwd a = {};
+  a.x = (const char*)x, a.stride = x_stride, a.vocab = (int)vocab, a.k = k, a.spans = sp.spans, a.span = sp.span;
+  a.targets = targets, a.logprob = logprob, a.entropy = entropy, a.stats = stats;
+  a.top_ids = top_ids, a.top_logprobs = top_logprobs, a.first_bad = (unsigned long long*)first_bad;
+  a.part = (float4*)workspace;
+  a.lists = (uint64_t*)((char*)workspace + dmt_align_up(sizeof(float4) * (size_t)rows * sp.spans, 256));
+  auto go = [&](auto spans, auto join) {
+    hipLaunchKernelGGL(spans, dim3((unsigned)(rows * sp.spans)), dim3(kBlock), 0, (hipStream_t)stream, a);
+    if (sp.spans > 1) hipLaunchKernelGGL(join, dim3((unsigned)rows), dim3(kBlock), 0, (hipStream_t)stream, a);
   };
-  if (dtype == DMT_F32) go(logprob_fwd<DMT_F32>);
-  else if (dtype == DMT_F16) go(logprob_fwd<DMT_F16>);
-  else go(logprob_fwd<DMT_BF16>);
+  auto type = [&](auto top) {
+    constexpr bool Top = decltype(top)::value;
+    if (dtype == DMT_F32) go(logprob_spans<DMT_F32, Top>, logprob_join<DMT_F32, Top>);
+    else if (dtype == DMT_F16) go(logprob_spans<DMT_F16, Top>, logprob_join<DMT_F16, Top>);
+    else go(logprob_spans<DMT_BF16, Top>, logprob_join<DMT_BF16, Top>);
+  };
+  if (k > 0) type(std::true_type());
+  else type(std::false_type());
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }
 
@@ -163,9 +449,12 @@ extern "C" dmt_status dmt_token_logprob_bwd(const void* x, int64_t rows, int64_t
   if (x == dx && x_stride != dx_stride && rows > 1) return DMT_EINVAL;
   if (!fits(rows, vocab)) return DMT_ENOTSUP;
   if (rows == 0) return DMT_OK;
+  const int64_t piece = dtype == DMT_F32 ? piece_elems<DMT_F32>() : piece_elems<DMT_BF16>();
+  const int64_t pieces = (vocab + piece - 1) / piece;
+  if (rows * pieces >= (1ll << 31)) return DMT_ENOTSUP;
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kBlock), 0, (hipStream_t)stream, (const char*)x, (int)vocab,
-                       x_stride, targets, stats, entropy, grad_logprob, grad_entropy, (char*)dx, dx_stride);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * pieces)), dim3(kBlock), 0, (hipStream_t)stream, (const char*)x,
+                       (int)vocab, x_stride, (int)pieces, targets, stats, entropy, grad_logprob, grad_entropy, (char*)dx, dx_stride);
   };
   if (dtype == DMT_F32) go(logprob_bwd<DMT_F32>);
   else if (dtype == DMT_F16) go(logprob_bwd<DMT_F16>);
