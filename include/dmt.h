@@ -571,7 +571,7 @@ dmt_status dmt_layer_norm_bwd(const void* x, int64_t rows, int64_t cols, int64_t
  *   k        0 ... DMT_TOP_MAX (0: no top items; may exceed vocab)
  *   workspace of the size for (rows, vocab, k); one sized for more rows serves fewer
  * vocab >= 1, rows >= 0; DMT_ENOTSUP for rows beyond 2^31 - 1, vocab beyond 2^30 or more than 2^31 - 1
- * pieces of 4096 scores in all.
+ * pieces of 2048 scores in all.
  */
 #define DMT_TOP_MAX 64
 size_t dmt_token_logprob_workspace_bytes(int64_t rows, int64_t vocab, int32_t k);

@@ -56,8 +56,8 @@ template <int DT, int E> struct Raw {
   uint32_t w[kWords];
 };
 
-// The first `valid` of them are there (valid >= 1 .. E; the others read as zero).
-template <int DT, int E>
+// The first `valid` of them are there (valid >= 1 .. E; the others read as zero).  Once: the line is not read again soon.
+template <int DT, int E, bool Once = false>
 __device__ __forceinline__ Raw<DT, E> load_raw(const char* p, int valid) {
   constexpr int EB = EltBytes<DT>::value, W = Raw<DT, E>::kWords;
   Raw<DT, E> r;
@@ -68,7 +68,8 @@ __device__ __forceinline__ Raw<DT, E> load_raw(const char* p, int valid) {
     } else {
 #pragma unroll
       for (int q = 0; q < W; q += 4) {
-        const dmt_u32x4 v = *(const DMT_GLOBAL typename Piece<EB>::v4*)(p + q * 4);
+        const DMT_GLOBAL typename Piece<EB>::v4* at = (const DMT_GLOBAL typename Piece<EB>::v4*)(p + q * 4);
+        const dmt_u32x4 v = Once ? __builtin_nontemporal_load(at) : *at;
         r.w[q] = v.x, r.w[q + 1] = v.y, r.w[q + 2] = v.z, r.w[q + 3] = v.w;
       }
     }
@@ -77,9 +78,10 @@ __device__ __forceinline__ Raw<DT, E> load_raw(const char* p, int valid) {
     for (int q = 0; q < W; ++q) r.w[q] = 0;
 #pragma unroll
     for (int i = 0; i < E - 1; ++i) {
-      if (i >= valid) break;
-      if constexpr (EB == 4) r.w[i] = *(const DMT_GLOBAL uint32_t*)(p + i * 4);
-      else r.w[i / 2] |= (uint32_t) * (const DMT_GLOBAL uint16_t*)(p + i * 2) << (i % 2 * 16);
+      if (i < valid) {
+        if constexpr (EB == 4) r.w[i] = *(const DMT_GLOBAL uint32_t*)(p + i * 4);
+        else r.w[i / 2] |= (uint32_t) * (const DMT_GLOBAL uint16_t*)(p + i * 2) << (i % 2 * 16);
+      }
     }
   }
   return r;
@@ -126,22 +128,47 @@ __device__ __forceinline__ void store_elems(char* p, int valid, const float (&x)
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < E - 1; ++i) {
-      if (i >= valid) break;
-      store1<DT>(p + i * EB, x[i]);
-    }
+    for (int i = 0; i < E - 1; ++i)
+      if (i < valid) store1<DT>(p + i * EB, x[i]);
   }
 }
 
-// Sum over the lanes of an aligned group of G lanes, the same in each of them.
+// Lane ^ O's value, O a power of two below 64: by DPP inside a row of 16 lanes, by gfx950's row and half swaps
+// across them (no trip through LDS, which a shuffle is).
+template <int O> __device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+  if constexpr (O == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true);         // quad_perm 1 0 3 2
+  else if constexpr (O == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true);    // quad_perm 2 3 0 1
+  else if constexpr (O == 4)                                                              // ^ 7, then ^ 3
+    return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true), 0x1B, 0xf, 0xf, true);
+  else if constexpr (O == 8) return __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);   // row_ror 8
+  else if constexpr (O == 16) {
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);                  // rows 0 0 2 2, 1 1 3 3
+    return threadIdx.x & 16 ? p[0] : p[1];
+  } else {
+    const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);                  // low low, high high
+    return threadIdx.x & 32 ? p[0] : p[1];
+  }
+}
+template <int O> __device__ __forceinline__ float lane_xor(float v) {
+  return __uint_as_float(lane_xor<O>(__float_as_uint(v)));
+}
+template <int O> __device__ __forceinline__ uint64_t lane_xor(uint64_t v) {
+  return (uint64_t)lane_xor<O>((uint32_t)(v >> 32)) << 32 | lane_xor<O>((uint32_t)v);
+}
+
+// Sum (maximum) over the lanes of an aligned group of G lanes, the same in each of them.
 template <int G> __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  if constexpr (G > 1) {
+    v = group_sum<G / 2>(v);
+    v += lane_xor<G / 2>(v);
+  }
   return v;
 }
 template <int G> __device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-  for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  if constexpr (G > 1) {
+    v = group_max<G / 2>(v);
+    v = fmaxf(v, lane_xor<G / 2>(v));
+  }
   return v;
 }
 

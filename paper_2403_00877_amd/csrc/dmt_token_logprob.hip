@@ -1,7 +1,7 @@
 // dmt_token_logprob_fwd, dmt_token_logprob_bwd: rows of scores as distributions.
 //   M = max x, S = sum exp(x - M), T = sum exp(x - M) (x - M):  log p_j = x_j - M - log S,  H = log S - T / S.
 //
-// Forward, one pass over the scores.  A block takes a span of a row, 16 KB at a time in registers; every lane keeps a maximum, S
+// Forward, one pass over the scores.  A block takes a span of a row, 8 KB at a time in registers; every lane keeps a maximum, S
 // and T of its own and rescales them when its maximum grows.  Exponents are kept to the base 2: z = x log2 e - M log2 e is one
 // fused multiply-add, and M's product is rounded once and the same in every term (and in the backward), so its error cancels.
 // The top k: each wave holds its 64 best so far, sorted, one a lane.  The k-th largest of the lanes' maxima of a piece is a
@@ -16,7 +16,7 @@
 namespace {
 
 constexpr int kBlock = 256, kWaves = kBlock / 64;
-constexpr int kVecs = 4;                                   // 16-byte pieces of a lane under way
+constexpr int kVecs = 2;                                   // 16-byte pieces of a lane under way
 constexpr float kInf = __builtin_inff();
 constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 constexpr float kFar = 1e30f;                              // |M| beyond which M log2 e may overflow
@@ -64,30 +64,33 @@ __device__ __forceinline__ float entry_score(uint64_t e) {
 __device__ __forceinline__ uint32_t entry_item(uint64_t e) { return 0xffffffffu - (uint32_t)e; }
 
 template <typename V> __device__ __forceinline__ V larger(V a, V b) { return a > b ? a : b; }
-template <typename V> __device__ __forceinline__ V smaller(V a, V b) { return a > b ? b : a; }
 
+// One step of a bitonic network: lanes O apart, those with KEEP's bit set take the larger value.
+template <int O, uint64_t KEEP, typename V> __device__ __forceinline__ V exchange(V v) {
+  const V w = dmt::lane_xor<O>(v);
+  return __builtin_amdgcn_inverse_ballot_w64(KEEP) == (v > w) ? v : w;
+}
+// The lanes whose bit N is 0.
+constexpr uint64_t lanes_without(int n) {
+  uint64_t m = 0;
+  for (int i = 0; i < 64; ++i) m |= (uint64_t)((i & n) == 0) << i;
+  return m;
+}
 // A sequence that rises, then falls (or the other way round) into falling order.
-template <typename V> __device__ __forceinline__ V merge_falling(V v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const V w = __shfl_xor(v, o);
-    v = lane & o ? smaller(v, w) : larger(v, w);
-  }
+template <int O = 32, typename V> __device__ __forceinline__ V merge_falling(V v) {
+  v = exchange<O, lanes_without(O)>(v);
+  if constexpr (O > 1) v = merge_falling<O / 2>(v);
   return v;
 }
-template <typename V, bool Falling> __device__ __forceinline__ V sort64(V v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int n = 2; n <= 64; n *= 2)
-#pragma unroll
-    for (int o = n / 2; o > 0; o >>= 1) {
-      const V w = __shfl_xor(v, o);
-      const bool low = (lane & o) == 0, falling = ((lane & n) == 0) == Falling;
-      v = low == falling ? larger(v, w) : smaller(v, w);
-    }
-  return v;
+// Blocks of N lanes (rising and falling by turns) into such blocks of 2 N ... 64.
+template <bool Falling, int N, int O, typename V> __device__ __forceinline__ V sort_steps(V v) {
+  constexpr uint64_t up = Falling ? lanes_without(N) : ~lanes_without(N);
+  v = exchange<O, ~(lanes_without(O) ^ up)>(v);
+  if constexpr (O > 1) return sort_steps<Falling, N, O / 2>(v);
+  else if constexpr (N < 64) return sort_steps<Falling, N * 2, N>(v);
+  else return v;
 }
+template <typename V, bool Falling> __device__ __forceinline__ V sort64(V v) { return sort_steps<Falling, 2, 1>(v); }
 // The 64 best of a falling list and of 64 entries in any order.
 __device__ __forceinline__ uint64_t add64(uint64_t list, uint64_t more) {
   return merge_falling(larger(list, sort64<uint64_t, false>(more)));
@@ -162,11 +165,17 @@ __device__ __forceinline__ void finish(const Fwd& a, int64_t row, const Sum& all
   }
 }
 
-// 16 KB of a row from element j on, -inf behind `end`.
-template <int DT>
+// 8 KB of a row from element j on, -inf behind `end`.
+template <int DT, bool Once = false>
 __device__ __forceinline__ void load_piece(const char* row, int j, int end, dmt::Raw<DT, dmt::ChunkElems<DT>::value> (&r)[kVecs]) {
   constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value, W = dmt::Raw<DT, E>::kWords;
   constexpr uint32_t kMasked = DT == DMT_F32 ? 0xff800000u : DT == DMT_F16 ? 0xfc00fc00u : 0xff80ff80u;
+  if (j + piece_elems<DT>() <= end) {
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v)
+      r[v] = dmt::load_raw<DT, E, Once>(row + ((int64_t)j + (v * kBlock + (int)threadIdx.x) * E) * EB, E);
+    return;
+  }
 #pragma unroll
   for (int v = 0; v < kVecs; ++v) {
     const int at = j + (v * kBlock + (int)threadIdx.x) * E, valid = end - at;
@@ -185,11 +194,12 @@ __device__ __forceinline__ void load_piece(const char* row, int j, int end, dmt:
   }
 }
 
-template <int DT, bool Top>
-__global__ __launch_bounds__(kBlock) void logprob_spans(const Fwd a) {
+// Once: the scores pass the caches by.
+template <int DT, bool Top, bool Once>
+__global__ __launch_bounds__(kBlock, 5) void logprob_spans(const Fwd a) {
   constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
   __shared__ float s_sum[kWaves][3];
-  __shared__ uint64_t s_list[kWaves][128];                 // candidates of each wave; its list at the end
+  __shared__ uint64_t s_list[kWaves][Top ? 64 + 64 * E : 64];   // each wave's candidates: less than 64 and a vector's; its list at the end
   const int64_t row = blockIdx.x / (unsigned)a.spans;
   const int span = (int)(blockIdx.x % (unsigned)a.spans);
   const char* x = a.x + row * a.stride * EB;
@@ -200,20 +210,18 @@ __global__ __launch_bounds__(kBlock) void logprob_spans(const Fwd a) {
   float cut = -kInf;                                       // scores up to it are not among the k best
   int waiting = 0;
   uint64_t* buf = s_list[wave];
-  // takes up to 64 of the waiting candidates into the list
-  auto take = [&]() {
-    const int from = max(0, waiting - 64);
-    const uint64_t e = from + lane < waiting ? buf[from + lane] : 0;
-    __builtin_amdgcn_wave_barrier();
-    waiting = from;
-    list = add64(list, e);
-  };
+  // The next piece is requested ahead (with the lists beside it that costs more waves than it gains: 58 us for 55).
+  constexpr bool Ahead = !Top;
   dmt::Raw<DT, E> r[kVecs], next[kVecs];
-  load_piece<DT>(x, begin, end, next);
+  if (Ahead) load_piece<DT, Once>(x, begin, end, next);
   for (int j = begin; j < end; j += piece_elems<DT>()) {
+    if constexpr (Ahead) {
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v) r[v] = next[v];
-    if (j + piece_elems<DT>() < end) load_piece<DT>(x, j + piece_elems<DT>(), end, next);
+      for (int v = 0; v < kVecs; ++v) r[v] = next[v];
+      if (j + piece_elems<DT>() < end) load_piece<DT, Once>(x, j + piece_elems<DT>(), end, next);
+    } else {
+      load_piece<DT, Once>(x, j, end, r);
+    }
     float most[kVecs], pm = -kInf;
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
@@ -243,7 +251,8 @@ __global__ __launch_bounds__(kBlock) void logprob_spans(const Fwd a) {
     else add([&](float v) { return fmaf(v, kLog2e, -m2); });
     if constexpr (Top) {
       const uint64_t over = __ballot(pm > cut);
-      if (over) {
+      const bool last = j + piece_elems<DT>() >= end;
+      if (over || (last && waiting > 0)) {
         float low = cut;                                   // of this piece, candidates are above it
         if (__popcll(over) >= a.k) {
           // at least k scores reach the k-th largest of the lanes' maxima; equal ones may have lower items
@@ -252,31 +261,39 @@ __global__ __launch_bounds__(kBlock) void logprob_spans(const Fwd a) {
           const float below = bound == 0.f ? -__uint_as_float(1u) : __uint_as_float(bound > 0.f ? u - 1 : u + 1);
           low = fmaxf(low, bound == -kInf ? bound : below);
         }
-#pragma unroll
+        // (a real loop, the pieces handed down: the sort in it is hundreds of instructions)
+#pragma unroll 1
         for (int v = 0; v < kVecs; ++v) {
-          if (!__any(most[v] > low)) continue;
-          float e[E];
-          dmt::unpack<DT, E>(r[v], e);
+          if (__any(most[0] > low)) {
+            float e[E];
+            dmt::unpack<DT, E>(r[0], e);
 #pragma unroll
-          for (int q = 0; q < E; ++q) {
-            const uint64_t mask = __ballot(e[q] > low);
-            if (!mask) continue;
-            if (mask >> lane & 1)
-              buf[waiting + __popcll(mask & ((1ull << lane) - 1))] =
-                  entry(e[q], (uint32_t)(j + (v * kBlock + (int)threadIdx.x) * E + q));
+            for (int q = 0; q < E; ++q) {
+              const uint64_t mask = __ballot(e[q] > low);
+              if (!mask) continue;
+              if (mask >> lane & 1)
+                buf[waiting + __popcll(mask & ((1ull << lane) - 1))] =
+                    entry(e[q], (uint32_t)(j + (v * kBlock + (int)threadIdx.x) * E + q));
+              waiting += __popcll(mask);
+            }
             __builtin_amdgcn_wave_barrier();
-            waiting += __popcll(mask);
-            if (waiting >= 64) take();
+          }
+#pragma unroll
+          for (int w = 0; w + 1 < kVecs; ++w) r[w] = r[w + 1], most[w] = most[w + 1];
+          // a full wave of them, or what there is after the first piece (for its bound) and the last
+          while (waiting >= 64 || (waiting > 0 && v == kVecs - 1 && (last || j == begin))) {
+            const int from = max(0, waiting - 64);
+            const uint64_t e = from + lane < waiting ? buf[from + lane] : 0;
+            __builtin_amdgcn_wave_barrier();
+            waiting = from;
+            list = add64(list, e);
           }
         }
-        if (waiting > 0 && (j == begin || j + piece_elems<DT>() >= end)) take();
         // later pieces hold later items only: a score has to beat the k-th
-        const float kth = __shfl(entry_score(list), a.k - 1);
-        cut = fmaxf(cut, kth);
+        cut = fmaxf(cut, __shfl(entry_score(list), a.k - 1));
       }
     }
   }
-  if (Top && waiting > 0) take();
   sum = join_sums(sum, s_sum);
   if constexpr (Top) list = join_lists(list, (uint64_t(*)[64])s_list);
   if (a.spans == 1) {
@@ -370,6 +387,7 @@ struct Spans {
   int spans, span;
 };
 constexpr int64_t kFillBlocks = 2048;
+constexpr int64_t kCacheBytes = 256 << 20;
 Spans spans_of(int64_t rows, int64_t vocab, int64_t piece) {
   const int64_t pieces = (vocab + piece - 1) / piece;
   const int64_t want = std::min(pieces, std::max<int64_t>(1, (kFillBlocks + rows - 1) / std::max<int64_t>(rows, 1)));
@@ -422,14 +440,18 @@ extern "C" dmt_status dmt_token_logprob_fwd(const void* x, int64_t rows, int64_t
     hipLaunchKernelGGL(spans, dim3((unsigned)(rows * sp.spans)), dim3(kBlock), 0, (hipStream_t)stream, a);
     if (sp.spans > 1) hipLaunchKernelGGL(join, dim3((unsigned)rows), dim3(kBlock), 0, (hipStream_t)stream, a);
   };
-  auto type = [&](auto top) {
-    constexpr bool Top = decltype(top)::value;
-    if (dtype == DMT_F32) go(logprob_spans<DMT_F32, Top>, logprob_join<DMT_F32, Top>);
-    else if (dtype == DMT_F16) go(logprob_spans<DMT_F16, Top>, logprob_join<DMT_F16, Top>);
-    else go(logprob_spans<DMT_BF16, Top>, logprob_join<DMT_BF16, Top>);
+  auto type = [&](auto top, auto once) {
+    constexpr bool Top = decltype(top)::value, Once = decltype(once)::value;
+    if (dtype == DMT_F32) go(logprob_spans<DMT_F32, Top, Once>, logprob_join<DMT_F32, Top>);
+    else if (dtype == DMT_F16) go(logprob_spans<DMT_F16, Top, Once>, logprob_join<DMT_F16, Top>);
+    else go(logprob_spans<DMT_BF16, Top, Once>, logprob_join<DMT_BF16, Top>);
   };
-  if (k > 0) type(std::true_type());
-  else type(std::false_type());
+  // Scores that the Infinity Cache does not hold for the backward need not pass through it: 1 GiB, forward 239 -> 212 us (its
+  // backward 348 -> 363); 64 MiB would be 17.0 for 17.0 and the backward 22.8 for 21.6.
+  const bool once = (double)rows * (double)vocab * (double)dmt_ebytes(dtype) > (double)kCacheBytes;
+  if (k > 0) type(std::true_type(), std::false_type());
+  else if (once) type(std::false_type(), std::true_type());
+  else type(std::false_type(), std::false_type());
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }
 
