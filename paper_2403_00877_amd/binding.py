@@ -165,8 +165,14 @@ def _check(where: str, code: int) -> None:
         raise DmtError(where, code)
 
 
-def _stream(stream) -> Optional[int]:
+# The current stream's handle without a Stream object around it (which takes 2.8 us, more than most kernels' launch).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
@@ -484,15 +490,19 @@ def dmt_plan_set_row_shards(plan: dmt_plan, row_begin: Sequence[int]) -> None:
 
 def _rows(t: torch.Tensor, rows: int, cols: int, dtype=None) -> int:
     """Row stride in elements of a [rows][cols] matrix."""
-    assert t.is_cuda and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols, (tuple(t.shape), rows, cols)
+    assert t.is_cuda and t.shape == (rows, cols), (t.device, tuple(t.shape), rows, cols)
     assert dtype is None or t.dtype == dtype, (t.dtype, dtype)
-    assert cols == 1 or t.stride(1) == 1, t.stride()
-    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    stride, one = t.stride()
+    assert one == 1 or cols == 1, (stride, one)
+    return stride if rows > 1 else max(cols, stride)
 
 
-def _vec(t: Optional[torch.Tensor], n: int, dtype) -> None:
-    assert t is None or (t.is_cuda and t.is_contiguous() and t.numel() == n and t.dtype == dtype), \
-        (tuple(t.shape), t.dtype, n, dtype)
+def _vec(t: Optional[torch.Tensor], n: int, dtype) -> Optional[int]:
+    """Address of n contiguous elements (None: of nothing)."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == dtype and t.numel() == n and t.is_contiguous(), (tuple(t.shape), t.dtype, n, dtype)
+    return t.data_ptr()
 
 
 def dmt_embed_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
@@ -500,11 +510,10 @@ def dmt_embed_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, sca
     """out[i] = scale * table[ids[i]]; ids int32, any shape; out [ids.numel()][table's columns]."""
     rows, cols = table.shape
     n = ids.numel()
-    _vec(ids, n, torch.int32)
-    _vec(first_bad, 1, torch.int64)
     _check("dmt_embed_fwd", _lib.dmt_embed_fwd(
-        _ptr(table), rows, cols, _rows(table, rows, cols), DTYPE_CODE[table.dtype], _ptr(ids), n, scale,
-        _ptr(out), _rows(out, n, cols), DTYPE_CODE[out.dtype], _ptr(first_bad), _stream(stream)))
+        table.data_ptr(), rows, cols, _rows(table, rows, cols), DTYPE_CODE[table.dtype], _vec(ids, n, torch.int32), n,
+        scale, out.data_ptr(), _rows(out, n, cols), DTYPE_CODE[out.dtype], _vec(first_bad, 1, torch.int64),
+        _stream(stream)))
 
 
 def dmt_embed_bwd_workspace_bytes(n: int, rows: int, cols: int) -> int:
@@ -517,32 +526,29 @@ def dmt_embed_bwd(ids: torch.Tensor, grad: torch.Tensor, grad_table: torch.Tenso
     """grad_table (float32) = or += scale * the sum of grad's rows by id."""
     rows, cols = grad_table.shape
     n = ids.numel()
-    _vec(ids, n, torch.int32)
-    _vec(first_bad, 1, torch.int64)
     _check("dmt_embed_bwd", _lib.dmt_embed_bwd(
-        _ptr(ids), n, _ptr(grad), _rows(grad, n, cols), DTYPE_CODE[grad.dtype], scale, _ptr(grad_table), rows,
-        cols, _rows(grad_table, rows, cols, torch.float32), int(accumulate), _ptr(first_bad), _ptr(workspace),
-        _nbytes(workspace), _stream(stream)))
+        _vec(ids, n, torch.int32), n, grad.data_ptr(), _rows(grad, n, cols), DTYPE_CODE[grad.dtype], scale,
+        grad_table.data_ptr(), rows, cols, _rows(grad_table, rows, cols, torch.float32), accumulate,
+        _vec(first_bad, 1, torch.int64), workspace.data_ptr(), workspace.nbytes, _stream(stream)))
 
 
-def _weight_code(x: torch.Tensor, *weights: Optional[torch.Tensor]) -> int:
-    types = {w.dtype for w in weights if w is not None}
-    assert len(types) <= 1, types
+def _weights(x: torch.Tensor, *weights: Optional[torch.Tensor]):
+    """The weights' common type and their addresses."""
+    dtype, at = None, []
     for w in weights:
-        if w is not None:
-            _vec(w, x.shape[1], w.dtype)
-    return DTYPE_CODE[types.pop()] if types else DMT_F32
+        dtype = dtype if w is None or dtype is not None else w.dtype
+        at.append(_vec(w, x.shape[1], dtype))
+    return DMT_F32 if dtype is None else DTYPE_CODE[dtype], at
 
 
 def dmt_layer_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
                        y: torch.Tensor, mean: Optional[torch.Tensor] = None,
                        rstd: Optional[torch.Tensor] = None, stream=None) -> None:
     rows, cols = x.shape
-    _vec(mean, rows, torch.float32)
-    _vec(rstd, rows, torch.float32)
+    weight_code, (g, b) = _weights(x, gamma, beta)
     _check("dmt_layer_norm_fwd", _lib.dmt_layer_norm_fwd(
-        _ptr(x), rows, cols, _rows(x, rows, cols), DTYPE_CODE[x.dtype], _ptr(gamma), _ptr(beta),
-        _weight_code(x, gamma, beta), eps, _ptr(y), _rows(y, rows, cols, x.dtype), _ptr(mean), _ptr(rstd),
+        x.data_ptr(), rows, cols, _rows(x, rows, cols), DTYPE_CODE[x.dtype], g, b, weight_code, eps, y.data_ptr(),
+        _rows(y, rows, cols, x.dtype), _vec(mean, rows, torch.float32), _vec(rstd, rows, torch.float32),
         _stream(stream)))
 
 
@@ -555,12 +561,12 @@ def dmt_layer_norm_bwd(x: torch.Tensor, gamma: Optional[torch.Tensor], mean: tor
                        dbeta: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                        stream=None) -> None:
     rows, cols = x.shape
-    for t, n in ((mean, rows), (rstd, rows), (dgamma, cols), (dbeta, cols)):
-        _vec(t, n, torch.float32)
+    weight_code, (g,) = _weights(x, gamma)
     _check("dmt_layer_norm_bwd", _lib.dmt_layer_norm_bwd(
-        _ptr(x), rows, cols, _rows(x, rows, cols), DTYPE_CODE[x.dtype], _ptr(gamma), _weight_code(x, gamma),
-        _ptr(mean), _ptr(rstd), _ptr(dy), _rows(dy, rows, cols), DTYPE_CODE[dy.dtype], _ptr(dx),
-        _rows(dx, rows, cols, dy.dtype), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), _nbytes(workspace),
+        x.data_ptr(), rows, cols, _rows(x, rows, cols), DTYPE_CODE[x.dtype], g, weight_code,
+        _vec(mean, rows, torch.float32), _vec(rstd, rows, torch.float32), dy.data_ptr(), _rows(dy, rows, cols),
+        DTYPE_CODE[dy.dtype], dx.data_ptr(), _rows(dx, rows, cols, dy.dtype), _vec(dgamma, cols, torch.float32),
+        _vec(dbeta, cols, torch.float32), None if workspace is None else workspace.data_ptr(), _nbytes(workspace),
         _stream(stream)))
 
 
@@ -576,31 +582,23 @@ def dmt_token_logprob_fwd(x: torch.Tensor, targets: Optional[torch.Tensor] = Non
     """k is top_ids' second size."""
     rows, vocab = x.shape
     k = 0 if top_ids is None else top_ids.shape[1]
-    _vec(targets, rows, torch.int32)
-    _vec(logprob, rows, torch.float32)
-    _vec(entropy, rows, torch.float32)
-    _vec(stats, 2 * rows, torch.float32)
-    _vec(top_ids, rows * k, torch.int32)
-    _vec(top_logprobs, rows * k, torch.float32)
-    _vec(first_bad, 1, torch.int64)
+    f32, i32 = torch.float32, torch.int32
     _check("dmt_token_logprob_fwd", _lib.dmt_token_logprob_fwd(
-        _ptr(x), rows, vocab, _rows(x, rows, vocab), DTYPE_CODE[x.dtype], _ptr(targets), _ptr(logprob),
-        _ptr(entropy), _ptr(stats), k, _ptr(top_ids), _ptr(top_logprobs), _ptr(first_bad), _ptr(workspace),
-        _nbytes(workspace), _stream(stream)))
+        x.data_ptr(), rows, vocab, _rows(x, rows, vocab), DTYPE_CODE[x.dtype], _vec(targets, rows, i32),
+        _vec(logprob, rows, f32), _vec(entropy, rows, f32), _vec(stats, 2 * rows, f32), k, _vec(top_ids, rows * k, i32),
+        _vec(top_logprobs, rows * k, f32), _vec(first_bad, 1, torch.int64),
+        None if workspace is None else workspace.data_ptr(), _nbytes(workspace), _stream(stream)))
 
 
 def dmt_token_logprob_bwd(x: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor,
                           entropy: Optional[torch.Tensor], grad_logprob: Optional[torch.Tensor],
                           grad_entropy: Optional[torch.Tensor], dx: torch.Tensor, stream=None) -> None:
     rows, vocab = x.shape
-    _vec(targets, rows, torch.int32)
-    _vec(stats, 2 * rows, torch.float32)
-    for t in (entropy, grad_logprob, grad_entropy):
-        _vec(t, rows, torch.float32)
+    f32 = torch.float32
     _check("dmt_token_logprob_bwd", _lib.dmt_token_logprob_bwd(
-        _ptr(x), rows, vocab, _rows(x, rows, vocab), DTYPE_CODE[x.dtype], _ptr(targets), _ptr(stats),
-        _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(dx), _rows(dx, rows, vocab, x.dtype),
-        _stream(stream)))
+        x.data_ptr(), rows, vocab, _rows(x, rows, vocab), DTYPE_CODE[x.dtype], _vec(targets, rows, torch.int32),
+        _vec(stats, 2 * rows, f32), _vec(entropy, rows, f32), _vec(grad_logprob, rows, f32),
+        _vec(grad_entropy, rows, f32), dx.data_ptr(), _rows(dx, rows, vocab, x.dtype), _stream(stream)))
 
 
 def make_grad_list(tensors: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None):
@@ -621,13 +619,11 @@ def dmt_grad_norm_workspace_bytes(grad_list) -> int:
 
 
 def dmt_grad_norm(grad_list, norm: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
-    _vec(norm, 1, torch.float32)
-    _check("dmt_grad_norm", _lib.dmt_grad_norm(grad_list, len(grad_list), _ptr(norm), _ptr(workspace),
-                                               _nbytes(workspace), _stream(stream)))
+    _check("dmt_grad_norm", _lib.dmt_grad_norm(grad_list, len(grad_list), _vec(norm, 1, torch.float32),
+                                               workspace.data_ptr(), workspace.nbytes, _stream(stream)))
 
 
 def dmt_grad_clip(grad_list, max_norm: float, norm: Optional[torch.Tensor], workspace: torch.Tensor,
                   stream=None) -> None:
-    _vec(norm, 1, torch.float32)
-    _check("dmt_grad_clip", _lib.dmt_grad_clip(grad_list, len(grad_list), max_norm, _ptr(norm), _ptr(workspace),
-                                               _nbytes(workspace), _stream(stream)))
+    _check("dmt_grad_clip", _lib.dmt_grad_clip(grad_list, len(grad_list), max_norm, _vec(norm, 1, torch.float32),
+                                               workspace.data_ptr(), workspace.nbytes, _stream(stream)))

@@ -1,7 +1,10 @@
 // dmt_grad_norm, dmt_grad_clip: the 2-norm over many gradients, and the gradients scaled by what it says.
-// The tensors are cut into chunks; a block per chunk sums squares in float64, one block adds the chunks up in a
-// fixed order.  The tensors' addresses travel as kernel arguments: nothing is copied to the device and a
-// call may be captured.
+//
+// The tensors are cut into units of kUnit elements, and every block has a consecutive run of units (so most blocks stay inside one
+// tensor).  It sums squares in float64, one sum a block; the scaling's blocks each add those sums up again, in the same
+// order, rather than wait for a launch that does.  Bound by memory: the gradients are read, then read and
+// written; the scaling's blocks walk their run backwards, so that what was read last comes from the Infinity Cache.
+// The tensors' addresses travel as kernel arguments: nothing is copied to the device and a call may be captured.
 #include <algorithm>
 
 #include "dmt_internal.h"
@@ -10,129 +13,163 @@
 namespace {
 
 constexpr int kBlock = 256, kWaves = kBlock / 64;
-constexpr int64_t kChunk = 32768;                 // elements
+constexpr int64_t kUnit = 2048;
+constexpr int64_t kBlocks = 2048;                 // of a launch, at most, and sums
 constexpr int kTensors = 120;                     // of one launch: kernel arguments end at 4 KB
+constexpr int kVecs = 4;                          // 16-byte pieces of a thread under way
 
 struct Tensors {
   const char* in[kTensors];
   char* out[kTensors];
   int64_t numel_dt[kTensors];                     // elements << 2 | type
-  uint32_t first[kTensors + 1];                   // first chunk, of the launch's
+  uint32_t first[kTensors + 1];                   // first unit, of the launch's
   int32_t count;
+  uint32_t per;                                   // units of a block
 };
 static_assert(sizeof(Tensors) <= 4000, "kernel arguments");
 
-// The tensor of a launch's chunk.
-__device__ __forceinline__ int tensor_of(const Tensors& t, uint32_t chunk) {
-  int lo = 0, hi = t.count;                       // first[lo] <= chunk < first[hi]
+// Calls go(tensor, from, to) for the pieces of tensors in the block's run of units.
+template <bool Backwards, typename Go> __device__ __forceinline__ void each_piece(const Tensors& t, Go go) {
+  const uint32_t all = t.first[t.count], u0 = min(all, blockIdx.x * t.per), u1 = min(all, u0 + t.per);
+  if (u0 == u1) return;
+  const uint32_t start = Backwards ? u1 - 1 : u0;
+  int lo = 0, hi = t.count;                       // first[lo] <= start < first[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
-    if (t.first[mid] <= chunk) lo = mid;
+    if (t.first[mid] <= start) lo = mid;
     else hi = mid;
   }
-  return lo;
-}
-
-template <int DT>
-__device__ __forceinline__ double chunk_squares(const char* in, int64_t n) {
-  constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
-  double s = 0;
-  for (int64_t c = threadIdx.x * E; c < n; c += kBlock * E) {
-    float x[E];
-    dmt::load_elems<DT, E>(in + c * EB, (int)min((int64_t)E, n - c), x);
-#pragma unroll
-    for (int q = 0; q < E; ++q) s = fma((double)x[q], (double)x[q], s);
+  for (int i = lo; i >= 0 && i < t.count; i += Backwards ? -1 : 1) {
+    const uint32_t a = max(u0, t.first[i]), b = min(u1, t.first[i + 1]);
+    if (a >= b) break;
+    go(i, (int64_t)(a - t.first[i]) * kUnit, min((int64_t)(b - t.first[i]) * kUnit, t.numel_dt[i] >> 2));
   }
-  return s;
 }
 
-__device__ __forceinline__ double block_sum_f64(double v, double* smem) {
+template <int DT> __device__ __forceinline__ void squares(const char* in, int64_t from, int64_t to, double& s) {
+  constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
+  for (int64_t c0 = from; c0 < to; c0 += kBlock * E * kVecs) {
+    dmt::Raw<DT, E> r[kVecs];
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+      const int64_t c = c0 + (v * kBlock + (int)threadIdx.x) * E;
+      if (c < to) r[v] = dmt::load_raw<DT, E>(in + c * EB, (int)min((int64_t)E, to - c));
+    }
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+      if (c0 + (v * kBlock + (int)threadIdx.x) * E >= to) break;
+      float x[E];
+      dmt::unpack<DT, E>(r[v], x);
+#pragma unroll
+      for (int q = 0; q < E; ++q) s = fma((double)x[q], (double)x[q], s);
+    }
+  }
+}
+
+// Sum over the block, the same in every thread; of NW waves.
+template <int NW> __device__ __forceinline__ double block_sum_f64(double v, double* smem) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   if ((threadIdx.x & 63) == 0) smem[threadIdx.x >> 6] = v;
   __syncthreads();
   double s = 0;
-  for (int w = 0; w < (int)blockDim.x / 64; ++w) s += smem[w];
+#pragma unroll
+  for (int w = 0; w < NW; ++w) s += smem[w];
   return s;
 }
 
-__global__ __launch_bounds__(kBlock) void grad_squares(const Tensors t, double* __restrict__ part) {
+// part[block] = or += (launches behind the first) the squares of its run.
+__global__ __launch_bounds__(kBlock) void grad_squares(const Tensors t, int later, double* __restrict__ part) {
   __shared__ double sm[kWaves];
-  const int i = tensor_of(t, blockIdx.x);
-  const int dt = (int)(t.numel_dt[i] & 3);
-  const int64_t at = (int64_t)(blockIdx.x - t.first[i]) * kChunk, n = min(kChunk, (t.numel_dt[i] >> 2) - at);
-  double s;
-  if (dt == DMT_F32) s = chunk_squares<DMT_F32>(t.in[i] + at * 4, n);
-  else if (dt == DMT_F16) s = chunk_squares<DMT_F16>(t.in[i] + at * 2, n);
-  else s = chunk_squares<DMT_BF16>(t.in[i] + at * 2, n);
-  s = block_sum_f64(s, sm);
-  if (threadIdx.x == 0) part[blockIdx.x] = s;
-}
-
-__global__ __launch_bounds__(1024) void grad_norm_sum(const double* __restrict__ part, int64_t n, float* __restrict__ norm,
-                                                      float max_norm, float* __restrict__ coef) {
-  __shared__ double sm[16];
   double s = 0;
-  for (int64_t i = threadIdx.x; i < n; i += 1024) s += part[i];
-  s = block_sum_f64(s, sm);
-  if (threadIdx.x == 0) {
-    const float v = (float)sqrt(s), c = max_norm / (v + 1e-6f);
-    if (norm) *norm = v;
-    if (coef) *coef = c >= 1.f ? 1.f : c;         // (NaN stays)
-  }
+  each_piece<false>(t, [&](int i, int64_t from, int64_t to) {
+    const int dt = (int)(t.numel_dt[i] & 3);
+    if (dt == DMT_F32) squares<DMT_F32>(t.in[i], from, to, s);
+    else if (dt == DMT_F16) squares<DMT_F16>(t.in[i], from, to, s);
+    else squares<DMT_BF16>(t.in[i], from, to, s);
+  });
+  s = block_sum_f64<kWaves>(s, sm);
+  if (threadIdx.x == 0) part[blockIdx.x] = later ? part[blockIdx.x] + s : s;
 }
 
-template <int DT>
-__device__ __forceinline__ void chunk_scale(const char* in, char* out, int64_t n, float c) {
+// The norm from `n` sums, the same in every thread of the block.
+__device__ __forceinline__ float norm_of(const double* __restrict__ part, int n, double* smem) {
+  double s = 0;
+  for (int i = threadIdx.x; i < n; i += kBlock) s += part[i];
+  return (float)sqrt(block_sum_f64<kWaves>(s, smem));
+}
+
+__global__ __launch_bounds__(kBlock) void grad_norm(const double* __restrict__ part, int n, float* __restrict__ norm) {
+  __shared__ double sm[kWaves];
+  const float v = norm_of(part, n, sm);
+  if (threadIdx.x == 0) *norm = v;
+}
+
+template <int DT> __device__ __forceinline__ void scale(const char* in, char* out, int64_t from, int64_t to, float f) {
   constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
-  for (int64_t e = threadIdx.x * E; e < n; e += kBlock * E) {
-    const int valid = (int)min((int64_t)E, n - e);
-    float x[E];
-    dmt::load_elems<DT, E>(in + e * EB, valid, x);
+  constexpr int64_t step = (int64_t)kBlock * E * kVecs;
+  for (int64_t c0 = from + (to - from - 1) / step * step; c0 >= from; c0 -= step) {
+    dmt::Raw<DT, E> r[kVecs];
 #pragma unroll
-    for (int q = 0; q < E; ++q) x[q] *= c;
-    dmt::store_elems<DT, E>(out + e * EB, valid, x);
+    for (int v = 0; v < kVecs; ++v) {
+      const int64_t c = c0 + (v * kBlock + (int)threadIdx.x) * E;
+      if (c < to) r[v] = dmt::load_raw<DT, E>(in + c * EB, (int)min((int64_t)E, to - c));
+    }
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+      const int64_t c = c0 + (v * kBlock + (int)threadIdx.x) * E;
+      if (c >= to) break;
+      float x[E];
+      dmt::unpack<DT, E>(r[v], x);
+#pragma unroll
+      for (int q = 0; q < E; ++q) x[q] *= f;
+      dmt::store_elems<DT, E>(out + c * EB, (int)min((int64_t)E, to - c), x);
+    }
   }
 }
 
-__global__ __launch_bounds__(kBlock) void grad_scale(const Tensors t, const float* __restrict__ coef) {
-  const float c = *coef;
-  const int i = tensor_of(t, blockIdx.x);
-  if (c == 1.f && t.in[i] == t.out[i]) return;
-  const int dt = (int)(t.numel_dt[i] & 3);
-  const int64_t at = (int64_t)(blockIdx.x - t.first[i]) * kChunk, n = min(kChunk, (t.numel_dt[i] >> 2) - at);
-  if (dt == DMT_F32) chunk_scale<DMT_F32>(t.in[i] + at * 4, t.out[i] + at * 4, n, c);
-  else if (dt == DMT_F16) chunk_scale<DMT_F16>(t.in[i] + at * 2, t.out[i] + at * 2, n, c);
-  else chunk_scale<DMT_BF16>(t.in[i] + at * 2, t.out[i] + at * 2, n, c);
+__global__ __launch_bounds__(kBlock) void grad_scale(const Tensors t, const double* __restrict__ part, int n,
+                                                     float max_norm, float* __restrict__ norm) {
+  __shared__ double sm[kWaves];
+  const float v = norm_of(part, n, sm), q = max_norm / (v + 1e-6f), f = q >= 1.f ? 1.f : q;     // (NaN stays)
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = v;
+  each_piece<true>(t, [&](int i, int64_t from, int64_t to) {
+    if (f == 1.f && t.in[i] == t.out[i]) return;
+    const int dt = (int)(t.numel_dt[i] & 3);
+    if (dt == DMT_F32) scale<DMT_F32>(t.in[i], t.out[i], from, to, f);
+    else if (dt == DMT_F16) scale<DMT_F16>(t.in[i], t.out[i], from, to, f);
+    else scale<DMT_BF16>(t.in[i], t.out[i], from, to, f);
+  });
 }
 
-int64_t chunks_of(int64_t numel) { return (numel + kChunk - 1) / kChunk; }
+int64_t units_of(int64_t numel) { return (numel + kUnit - 1) / kUnit; }
 
-dmt_status check(const dmt_grad_tensor* t, int64_t count, bool outs, int64_t* chunks) {
+dmt_status check(const dmt_grad_tensor* t, int64_t count, bool outs, int64_t* units) {
   if (count < 0 || (count > 0 && !t)) return DMT_EINVAL;
   if (count > (1 << 20)) return DMT_ENOTSUP;
-  *chunks = 0;
+  *units = 0;
   for (int64_t i = 0; i < count; ++i) {
     if (t[i].numel < 0 || !dmt_is_dtype(t[i].dtype)) return DMT_EINVAL;
     if (t[i].numel > (1ll << 40)) return DMT_ENOTSUP;
     if (t[i].numel == 0) continue;
     const int64_t e = dmt_ebytes(t[i].dtype);
     if (!dmt_is_at(t[i].data, e) || (outs && !dmt_is_at(t[i].out, e))) return DMT_EINVAL;
-    *chunks += chunks_of(t[i].numel);
+    *units += units_of(t[i].numel);
   }
-  return *chunks < (1ll << 31) ? DMT_OK : DMT_ENOTSUP;
+  return *units < (1ll << 31) ? DMT_OK : DMT_ENOTSUP;
 }
 
-// Calls go(tensors, chunks of the launch, chunks before it) for every launch.
+// Calls go(tensors, number of the launch) for every launch.
 template <typename Go>
-void launches(const dmt_grad_tensor* t, int64_t count, Go go) {
+void launches(const dmt_grad_tensor* t, int64_t count, int64_t blocks, Go go) {
   Tensors a;
-  int64_t before = 0;
+  int launch = 0;
   a.count = 0;
   a.first[0] = 0;
   auto flush = [&]() {
-    if (a.count > 0) go(a, a.first[a.count], before);
-    before += a.first[a.count];
+    if (a.count == 0) return;
+    a.per = (uint32_t)((a.first[a.count] + blocks - 1) / blocks);
+    go(a, launch++);
     a.count = 0;
   };
   for (int64_t i = 0; i < count; ++i) {
@@ -141,7 +178,7 @@ void launches(const dmt_grad_tensor* t, int64_t count, Go go) {
     a.in[at] = (const char*)t[i].data;
     a.out[at] = (char*)t[i].out;
     a.numel_dt[at] = t[i].numel << 2 | t[i].dtype;
-    a.first[a.count] = a.first[at] + (uint32_t)chunks_of(t[i].numel);
+    a.first[a.count] = a.first[at] + (uint32_t)units_of(t[i].numel);
     if (a.count == kTensors) flush();
   }
   flush();
@@ -149,30 +186,32 @@ void launches(const dmt_grad_tensor* t, int64_t count, Go go) {
 
 dmt_status norm_run(const dmt_grad_tensor* t, int64_t count, float max_norm, float* norm, bool clip, void* workspace,
                     size_t workspace_bytes, hipStream_t s) {
-  int64_t chunks = 0;
-  const dmt_status ok = check(t, count, clip, &chunks);
+  int64_t units = 0;
+  const dmt_status ok = check(t, count, clip, &units);
   if (ok != DMT_OK) return ok;
+  const int64_t blocks = std::min(units, kBlocks);          // of every launch, and sums
   if (!dmt_is_at(workspace, 256)) return DMT_EINVAL;
-  if (workspace_bytes < sizeof(double) * (size_t)(chunks + 1)) return DMT_ENOMEM;
-  float* coef = (float*)workspace;
-  double* part = (double*)workspace + 1;
-  launches(t, count, [&](const Tensors& a, uint32_t n, int64_t before) {
-    hipLaunchKernelGGL(grad_squares, dim3(n), dim3(kBlock), 0, s, a, part + before);
+  if (workspace_bytes < sizeof(double) * (size_t)std::max<int64_t>(blocks, 1)) return DMT_ENOMEM;
+  double* part = (double*)workspace;
+  launches(t, count, blocks, [&](const Tensors& a, int launch) {
+    hipLaunchKernelGGL(grad_squares, dim3((unsigned)blocks), dim3(kBlock), 0, s, a, launch > 0, part);
   });
-  hipLaunchKernelGGL(grad_norm_sum, dim3(1), dim3(1024), 0, s, part, chunks, norm, max_norm, clip ? coef : nullptr);
-  if (clip)
-    launches(t, count, [&](const Tensors& a, uint32_t n, int64_t) {
-      hipLaunchKernelGGL(grad_scale, dim3(n), dim3(kBlock), 0, s, a, coef);
+  if (clip && units > 0)
+    launches(t, count, blocks, [&](const Tensors& a, int launch) {
+      hipLaunchKernelGGL(grad_scale, dim3((unsigned)blocks), dim3(kBlock), 0, s, a, part, (int)blocks, max_norm,
+                         launch == 0 ? norm : nullptr);
     });
+  else if (norm)
+    hipLaunchKernelGGL(grad_norm, dim3(1), dim3(kBlock), 0, s, part, (int)blocks, norm);
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }
 
 }  // namespace
 
 extern "C" size_t dmt_grad_norm_workspace_bytes(const dmt_grad_tensor* tensors, int64_t count) {
-  int64_t chunks = 0;
-  if (check(tensors, count, false, &chunks) != DMT_OK) return 0;
-  return sizeof(double) * (size_t)(chunks + 1);
+  int64_t units = 0;
+  if (check(tensors, count, false, &units) != DMT_OK) return 0;
+  return sizeof(double) * (size_t)std::max<int64_t>(1, std::min(units, kBlocks));
 }
 
 extern "C" dmt_status dmt_grad_norm(const dmt_grad_tensor* tensors, int64_t count, float* norm,
