@@ -49,7 +49,7 @@ __global__ __launch_bounds__(kBlock) void embed_fwd_kernel(
 // ------------------------------------------------------------------ rows that no id names
 
 // They are cleared by waves of blocks behind those of the sums and of the join, which are bound by latency where the
-// clearing is bound by the rate of stores.
+// clearing is bound by the rate of stores; they pass the caches by (sums and join 114 -> 93 us at 930 K rows of 512 bytes).
 struct Fill {
   const uint8_t* touched;
   float* out;
@@ -66,11 +66,10 @@ template <int Waves> __device__ __forceinline__ bool fill_block(const Fill& f) {
   const int lane = threadIdx.x & 63, sub = lane & ((1 << f.log2_lanes) - 1);
   const int64_t v0 = (f.first + (int64_t)(blockIdx.x - f.own_blocks) * Waves + (threadIdx.x >> 6)) * f.rows_per_wave;
   const uint64_t empty = __ballot(lane < f.rows_per_wave && v0 + lane < f.rows && !f.touched[v0 + lane]);
-  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
   for (int i = lane >> f.log2_lanes; i < f.rows_per_wave; i += 64 >> f.log2_lanes) {
     if (!(empty >> i & 1)) continue;
     for (int c = sub * 4; c < f.cols; c += 4 << f.log2_lanes)
-      dmt::store_elems<DMT_F32, 4>((char*)(f.out + (v0 + i) * f.out_stride + c), min(4, f.cols - c), zero);
+      dmt::clear_elems<4>((char*)(f.out + (v0 + i) * f.out_stride + c), f.cols - c);
   }
   return true;
 }
@@ -226,52 +225,102 @@ __global__ __launch_bounds__(kSortBlock) void embed_scatter(
     }
 }
 
-// Few lookups: the whole order in one launch.  A block owns a range of rows and looks at every id itself, twice:
-// first it counts, per wave (a wave has a consecutive share of the ids) and row, and how many ids lie below its
-// range; then every id of the range has its place.  Counts are 16 bits, so n stays below 65536.
+// Few lookups: the whole order in one launch.  A block owns a range of rows and looks at every id itself: it counts them,
+// per wave (a wave has a consecutive share of the ids) and row, and how many ids lie below its range; then every id of the range has
+// its place.  A wave notes the few ids it finds, in their order, and places those; only a wave that finds more than kNotes, which
+// the owner of a frequent row does, looks at its share again.  A lane reads four consecutive ids at a time.
+// Counts are 16 bits, so n stays below 65536.  The last block's range holds the absent ids, as row `rows`.
 //   lds [waves][range / 2], two rows a word: afterwards where each wave's share of a row ends, counted from the
 //   block's first record;  counted(pair of rows, count of either) once per pair;
-//   placed(ids below the range, place, key, position) once per id of the range
-constexpr int kFewUnroll = 8;
+//   placed(ids below the range, place, row, position) once per id of the range
+constexpr int kIdsLane = 4, kIdsWave = 64 * kIdsLane, kFewUnroll = 4, kNotes = 128;
 template <typename Counted, typename Placed>
 __device__ __forceinline__ void order_few(const int32_t* __restrict__ ids, int n, uint32_t rows, int range, uint32_t* lds,
-                                              unsigned long long* __restrict__ first_bad, Counted counted,
-                                              Placed placed) {
+                                          unsigned long long* __restrict__ first_bad, Counted counted,
+                                          Placed placed) {
   __shared__ uint32_t sm[kSortWaves];
   __shared__ uint32_t s_below;
+  __shared__ uint32_t s_notes[kSortWaves][kNotes];                      // row in the range << 16 | position
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, words = range / 2;
+  const uint64_t lower = (1ull << lane) - 1;
   const uint32_t first = blockIdx.x * (uint32_t)range;
+  const bool absent_too = first + (uint32_t)range > rows;                // (the last block)
   for (int i = threadIdx.x; i < words * kSortWaves; i += kSortBlock) lds[i] = 0;
   if (threadIdx.x == 0) s_below = 0;
   __syncthreads();
-  const int per = (n + kSortBlock - 1) / kSortBlock * 64;
-  const int j0 = wave * per, j1 = min(n, j0 + per);
+  const int per = (n + kSortWaves * kIdsWave - 1) / (kSortWaves * kIdsWave) * kIdsWave;
+  const int j0 = min(n, wave * per), j1 = min(n, j0 + per);
   uint32_t* mine = lds + wave * words;
-  auto keys = [&](int j, uint32_t (&key)[kFewUnroll]) {
+  // look(position of the first of a lane's four, their rows), 64 * 4 ids at a time
+  auto each = [&](auto look) {
+    for (int j = j0; j < j1; j += kFewUnroll * kIdsWave) {
+      uint32_t key[kFewUnroll][kIdsLane];
+      const bool whole = j + kFewUnroll * kIdsWave <= j1;
 #pragma unroll
-    for (int u = 0; u < kFewUnroll; ++u) {
-      const int at = j + u * 64 + lane;
-      key[u] = at < j1 ? (uint32_t)ids[at] : ~0u;
+      for (int u = 0; u < kFewUnroll; ++u) {
+        const int at = j + u * kIdsWave + lane * kIdsLane;
+        if (whole) {
+          const auto r = dmt::load_raw<DMT_F32, kIdsLane>((const char*)(ids + at), kIdsLane);
+#pragma unroll
+          for (int e = 0; e < kIdsLane; ++e) key[u][e] = r.w[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < kIdsLane; ++e) key[u][e] = at + e < j1 ? (uint32_t)ids[at + e] : ~0u;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kFewUnroll; ++u) {
+        const int at = j + u * kIdsWave + lane * kIdsLane;
+        if (absent_too) {                                               // (ids below 0 are large unsigned ones)
+#pragma unroll
+          for (int e = 0; e < kIdsLane; ++e) key[u][e] = at + e < j1 ? min(key[u][e], rows) : ~0u;
+        }
+        look(at, key[u]);
+      }
     }
   };
-  uint32_t below = 0;
-  for (int j = j0; j < j1; j += kFewUnroll * 64) {
-    uint32_t key[kFewUnroll];
-    keys(j, key);
+  uint32_t below = 0;                                                   // (of the wave)
+  int notes = 0;
+  each([&](int at, const uint32_t (&key)[kIdsLane]) {
+    uint64_t in[kIdsLane], any = 0;
+    int before = notes;
 #pragma unroll
-    for (int u = 0; u < kFewUnroll; ++u) {
-      const int at = j + u * 64 + lane;
-      if (at >= j1) continue;
-      if (blockIdx.x == 0 && first_bad && (int32_t)key[u] >= 0 && key[u] >= rows)
-        atomicMin(first_bad, (unsigned long long)at);
-      const uint32_t v = min(key[u], rows), d = v - first;              // (a negative id is a large unsigned one)
-      below += v < first;
-      if (d < (uint32_t)range) atomicAdd(&mine[d >> 1], 1u << (d & 1) * 16);
+    for (int e = 0; e < kIdsLane; ++e) {
+      below += __popcll(__ballot(key[e] < first));
+      in[e] = __ballot(key[e] - first < (uint32_t)range);
+      any |= in[e];
     }
-  }
+    if (!any) return;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o);
+    for (int e = 0; e < kIdsLane; ++e) {
+      before += __popcll(in[e] & lower);
+      notes += __popcll(in[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < kIdsLane; ++e) {
+      if (!in[e]) continue;
+      const uint32_t d = key[e] - first;
+      const bool here = in[e] >> lane & 1;
+      if (here && before < kNotes) s_notes[wave][before] = d << 16 | (uint32_t)(at + e);
+      before += here;
+      // of many at once, the first lane's row is counted for all lanes that have it: LDS adds to one address go one after another,
+      // and a row may have a tenth of all ids
+      uint32_t many = 1;
+      bool counts = here;
+      if (__popcll(in[e]) > 4) {
+        const int lead = __builtin_ctzll(in[e]);
+        const uint32_t row = __builtin_amdgcn_readlane(d, lead);
+        const uint64_t same = __ballot(d == row) & in[e];
+        if (lane == lead) many = (uint32_t)__popcll(same);
+        else counts = here && d != row;
+      }
+      if (counts) atomicAdd(&mine[d >> 1], many << (d & 1) * 16);
+    }
+  });
   if (lane == 0) atomicAdd(&s_below, below);
+  if (blockIdx.x == 0 && first_bad)
+    for (int j = threadIdx.x; j < n; j += kSortBlock)
+      if (ids[j] >= 0 && (uint32_t)ids[j] >= rows) atomicMin(first_bad, (unsigned long long)j);
   __syncthreads();
   // counts -> places inside the block's records
   uint32_t before = 0;
@@ -299,34 +348,64 @@ __device__ __forceinline__ void order_few(const int32_t* __restrict__ ids, int n
   }
   __syncthreads();
   uint16_t* place = (uint16_t*)mine;
-  for (int j = j0; j < j1; j += kFewUnroll * 64) {
-    uint32_t key[kFewUnroll];
-    keys(j, key);
-#pragma unroll
-    for (int u = 0; u < kFewUnroll; ++u) {
-      const int at = j + u * 64 + lane;
-      const uint32_t v = min(key[u], rows), d = v - first;
-      const bool here = at < j1 && d < (uint32_t)range;
-      uint64_t left = __ballot(here);
-      while (left) {                                                    // one row of the 64 ids at a time
+  if (notes <= kNotes) {
+    for (int i0 = 0; i0 < notes; i0 += 64) {
+      const int many = min(64, notes - i0);
+      const uint32_t note = s_notes[wave][i0 + min(lane, many - 1)], d = note >> 16;
+      for (uint64_t left = many < 64 ? (1ull << many) - 1 : ~0ull; left;) {       // one row at a time
         const uint32_t row = __builtin_amdgcn_readlane(d, __builtin_ctzll(left));
-        const uint64_t same = __ballot(here && d == row);
-        const uint32_t from = place[row];
+        const uint64_t same = __ballot(d == row) & left;
+        const uint32_t to = place[row];
         __builtin_amdgcn_wave_barrier();
-        if (here && d == row) {
-          placed(s_below, from + __popcll(same & ((1ull << lane) - 1)), v, (uint32_t)at);
-          place[row] = (uint16_t)(from + __popcll(same));               // (the same from every lane)
+        if (same >> lane & 1) {
+          placed(s_below, to + __popcll(same & lower), first + row, note & 0xffffu);
+          place[row] = (uint16_t)(to + __popcll(same));                 // (the same from every lane)
         }
         __builtin_amdgcn_wave_barrier();
         left &= ~same;
       }
     }
+    return;
   }
+  each([&](int at, const uint32_t (&key)[kIdsLane]) {
+    uint64_t left[kIdsLane], any = 0;
+#pragma unroll
+    for (int e = 0; e < kIdsLane; ++e) {
+      left[e] = __ballot(key[e] - first < (uint32_t)range);
+      any |= left[e];
+    }
+    while (any) {                                                       // one row of the 256 ids at a time
+      const int lead = __builtin_ctzll(any);
+      uint32_t row = 0;
+#pragma unroll
+      for (int e = kIdsLane - 1; e >= 0; --e)
+        if (left[e] >> lead & 1) row = __builtin_amdgcn_readlane(key[e] - first, lead);
+      uint64_t same[kIdsLane];
+      const uint32_t from = place[row];
+      uint32_t to = from, total = 0;                                    // positions rise by lane, then inside a lane
+      any = 0;
+#pragma unroll
+      for (int e = 0; e < kIdsLane; ++e) {
+        same[e] = __ballot(key[e] - first == row) & left[e];
+        to += __popcll(same[e] & lower);
+        total += __popcll(same[e]);
+        left[e] &= ~same[e];
+        any |= left[e];
+      }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int e = 0; e < kIdsLane; ++e)
+        if (same[e] >> lane & 1) placed(s_below, to++, key[e], (uint32_t)(at + e));
+      if (lane == 0) place[row] = (uint16_t)(from + total);
+      __builtin_amdgcn_wave_barrier();
+    }
+  });
 }
 
 constexpr int kFewRows = 4096;               // rows of a block, at most: counts of 16 waves take 128 KB
 constexpr int64_t kFewBlocks = 256;          // ... and the least number of blocks
-constexpr int64_t kFewNnz = 65535, kFewWork = 1 << 25;
+// The line to the radix sort, us, ids of Zipf's frequencies: 32768 21.6 for 30, 65535 43 for 33.  (Uniform 13 and 21.)
+constexpr int64_t kFewNnz = 45056, kFewWork = 1 << 25;
 __global__ __launch_bounds__(kSortBlock) void embed_sort_few(const int32_t* __restrict__ ids, int n, uint32_t rows, int range,
                                                              uint64_t* __restrict__ out, uint16_t* __restrict__ touched,
                                                              unsigned long long* __restrict__ first_bad) {
@@ -357,7 +436,7 @@ struct Sums {
   int64_t out_stride;
   int cols, part_cols, accumulate, log2_lpr, tile;
   int64_t ntiles;
-  int slices, log2_join;                     // log2 of the join's lanes per row
+  int slices, log2_join;                     // log2 of the join's lanes per row (and of the one launch's that clear one)
   float* part;
   Fill fill;
 };
@@ -595,22 +674,24 @@ __global__ __launch_bounds__(kSortBlock) void embed_bwd_few(const int32_t* __res
       }
     }
   };
+  if (!Add)                                  // (16 bytes a lane: halves of lines, past the caches, would cost twice)
+    for (int r = threadIdx.x >> a.log2_join; r < range && first + r < rows; r += kSortBlock >> a.log2_join) {
+      if (ends[r] != (r > 0 ? ends[r - 1] : 0)) continue;
+      for (int c = (threadIdx.x & ((1 << a.log2_join) - 1)) * 4; c < a.cols; c += 4 << a.log2_join)
+        dmt::clear_elems<4>((char*)(a.out + (first + r) * a.out_stride + c), a.cols - c);
+    }
   for (int r = group; r < range && first + r < rows; r += groups) {
     const int from = r > 0 ? ends[r - 1] : 0, to = ends[r];
     if (to - from > kFusedLong) {
       if (lane == 0) many[atomicAdd(&s_many, 1u)] = (uint16_t)r;        // (their order changes no sum)
       continue;
     }
-    if (Add && to == from) continue;
+    if (to == from) continue;
     for (int c = lane * E; c < a.cols; c += E << a.log2_lpr) {
       float acc[E];
 #pragma unroll
       for (int q = 0; q < E; ++q) acc[q] = 0.f;
       const int valid = Whole ? E : min(E, a.cols - c);
-      if (to == from) {
-        dmt::store_elems<DMT_F32, E>((char*)(a.out + (first + r) * a.out_stride + c), valid, acc);
-        continue;
-      }
       sum(from, to, c, valid, acc);
       write_row<E, Add>(a, first + r, c, valid, acc);
     }
@@ -786,6 +867,7 @@ template <int GD>
 void launch_fused(const Ws& w, Sums a, const int32_t* ids, int64_t* bad, hipStream_t s) {
   constexpr int E = dmt::ChunkElems<GD>::value;
   a.log2_lpr = log2_lanes(a.cols, E);
+  a.log2_join = log2_lanes(a.cols, 4);
   variants(a.cols % E == 0, a.accumulate, [&](auto whole, auto add) {
     auto kernel = embed_bwd_few<GD, decltype(whole)::value, decltype(add)::value>;
     static DmtPerDevice done;

@@ -403,9 +403,10 @@ __global__ __launch_bounds__(1024) void norm_bwd_sum(const float* __restrict__ p
 
 // ------------------------------------------------------------------ how a call is divided
 
-// Lanes of a row and pieces of a lane, from the 16-byte pieces of x a row has; run(T, NV) as types.
+// Lanes of a row and pieces of a lane, from the pieces of E elements of x a row has; run(T, NV) as types.  False: longer than the
+// 128 registers of a thread of 1024 hold beside the weights (16384 columns; backward 8192).
 template <int V> struct Int { static constexpr int value = V; };
-template <typename Run> bool fwd_shape(int64_t pieces, Run run) {
+template <int E, typename Run> bool fwd_shape(int64_t pieces, Run run) {
   if (pieces <= 16) run(Int<16>(), Int<1>());
   else if (pieces <= 64) run(Int<64>(), Int<1>());
   else if (pieces <= 128) run(Int<64>(), Int<2>());
@@ -413,18 +414,25 @@ template <typename Run> bool fwd_shape(int64_t pieces, Run run) {
   else if (pieces <= 256) run(Int<64>(), Int<4>());
   else if (pieces <= 512) run(Int<256>(), Int<2>());
   else if (pieces <= 1024) run(Int<256>(), Int<4>());
-  else if (pieces <= 4096) run(Int<1024>(), Int<4>());
+  else if (pieces <= 2048) run(Int<1024>(), Int<2>());
+  else if constexpr (E == 4) {
+    if (pieces > 4096) return false;
+    run(Int<1024>(), Int<4>());
+  }
   else return false;
   return true;
 }
-template <typename Run> bool bwd_shape(int64_t pieces, Run run) {
+template <int E, typename Run> bool bwd_shape(int64_t pieces, Run run) {
   if (pieces <= 16) run(Int<16>(), Int<1>());
   else if (pieces <= 64) run(Int<64>(), Int<1>());
   else if (pieces <= 128) run(Int<64>(), Int<2>());
   else if (pieces <= 256) run(Int<256>(), Int<1>());
   else if (pieces <= 512) run(Int<256>(), Int<2>());
   else if (pieces <= 1024) run(Int<1024>(), Int<1>());
-  else if (pieces <= 2048) run(Int<1024>(), Int<2>());
+  else if constexpr (E == 4) {
+    if (pieces > 2048) return false;
+    run(Int<1024>(), Int<2>());
+  }
   else return false;
   return true;
 }
@@ -462,7 +470,7 @@ extern "C" dmt_status dmt_layer_norm_fwd(const void* x, int64_t rows, int64_t co
   auto go = [&](auto xd) {
     constexpr int XD = decltype(xd)::value;
     const int64_t pieces = (cols + dmt::ChunkElems<XD>::value - 1) / dmt::ChunkElems<XD>::value;
-    const bool done = fwd_shape(pieces, [&](auto t, auto nv) {
+    const bool done = fwd_shape<dmt::ChunkElems<XD>::value>(pieces, [&](auto t, auto nv) {
       constexpr int T = decltype(t)::value, B = T < kBlock ? kBlock : T;
       const int64_t blocks = std::min((rows + B / T - 1) / (B / T), fwd_blocks(T));
       hipLaunchKernelGGL((norm_fwd<XD, T, decltype(nv)::value>), dim3((unsigned)blocks), dim3(B), 0, s, a);
@@ -484,7 +492,7 @@ template <int XD, int GD>
 static void bwd_run(Bwd a, float* dgamma, float* dbeta, hipStream_t s) {
   const int64_t pieces = (a.cols + dmt::ChunkElems<XD>::value - 1) / dmt::ChunkElems<XD>::value;
   int64_t parts = 0;
-  const bool done = bwd_shape(pieces, [&](auto t, auto nv) {
+  const bool done = bwd_shape<dmt::ChunkElems<XD>::value>(pieces, [&](auto t, auto nv) {
     constexpr int T = decltype(t)::value, B = T < kBlock ? kBlock : T;
     parts = std::min((a.rows + B / T - 1) / (B / T), bwd_blocks(T));
     if (parts > 0) hipLaunchKernelGGL((norm_bwd<XD, GD, T, decltype(nv)::value>), dim3((unsigned)parts), dim3(B), 0, s, a);

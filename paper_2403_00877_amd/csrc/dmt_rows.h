@@ -133,6 +133,19 @@ __device__ __forceinline__ void store_elems(char* p, int valid, const float (&x)
   }
 }
 
+// The first `valid` of E float32 zeros, past the caches.
+template <int E> __device__ __forceinline__ void clear_elems(char* p, int valid) {
+  const dmt_u32x4 zero = {0, 0, 0, 0};
+  if (valid >= E) {
+#pragma unroll
+    for (int q = 0; q < E; q += 4) __builtin_nontemporal_store(zero, (DMT_GLOBAL Piece<4>::v4*)(p + q * 4));
+  } else {
+#pragma unroll
+    for (int i = 0; i < E - 1; ++i)
+      if (i < valid) store1<DMT_F32>(p + i * 4, 0.f);
+  }
+}
+
 // Lane ^ O's value, O a power of two below 64: by DPP inside a row of 16 lanes, by gfx950's row and half swaps
 // across them (no trip through LDS, which a shuffle is).
 template <int O> __device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
