@@ -52,7 +52,8 @@ __device__ __forceinline__ void rescale(Sum& a, float m) {
 
 // ------------------------------------------------------------------ sorted lists, one entry a lane
 
-// An entry orders by score, then by the lower item: larger entries are better, 0 is none.
+// An entry orders by score, then by the lower item: larger entries are better, 0 is none.  Between spans it is the float32 score
+// and the item, 64 bits; inside a span of 16-bit scores the score itself and the item's distance from the span's begin, 32 bits.
 __device__ __forceinline__ uint64_t entry(float v, uint32_t item) {
   const uint32_t u = __float_as_uint(v == 0.f ? 0.f : v);  // (zeros of both signs tie)
   return (uint64_t)((u >> 31) ? ~u : u | 0x80000000u) << 32 | (0xffffffffu - item);
@@ -62,6 +63,31 @@ __device__ __forceinline__ float entry_score(uint64_t e) {
   return e == 0 ? -kInf : __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u);
 }
 __device__ __forceinline__ uint32_t entry_item(uint64_t e) { return 0xffffffffu - (uint32_t)e; }
+
+template <int DT> struct Local {                           // inside a span
+  static constexpr int kMost = 65536;                      // scores of a span, at most
+  using type = uint32_t;
+  static __device__ __forceinline__ type make(float v, int at) {
+    uint32_t u = v == 0.f ? 0u : dmt::round2<DT>(v, 0.f) & 0xffffu;
+    return ((u >> 15) ? ~u & 0xffffu : u | 0x8000u) << 16 | (0xffffu - (uint32_t)at);
+  }
+  static __device__ __forceinline__ float score(type e) {
+    const uint32_t u = e >> 16, bits = (u >> 15) ? u & 0x7fffu : ~u & 0xffffu;
+    if (e == 0) return -kInf;
+    if constexpr (DT == DMT_BF16) return dmt::bf16_lo(bits);
+    else return dmt::f16_bits_to_f32(bits);
+  }
+  static __device__ __forceinline__ uint64_t wide(type e, int begin) {
+    return e ? entry(score(e), (uint32_t)begin + 0xffffu - (e & 0xffffu)) : 0;
+  }
+};
+template <> struct Local<DMT_F32> {
+  static constexpr int kMost = 1 << 30;
+  using type = uint64_t;
+  static __device__ __forceinline__ type make(float v, int at) { return entry(v, (uint32_t)at); }
+  static __device__ __forceinline__ float score(type e) { return entry_score(e); }
+  static __device__ __forceinline__ uint64_t wide(type e, int begin) { return e ? e - (uint32_t)begin : 0; }
+};
 
 template <typename V> __device__ __forceinline__ V larger(V a, V b) { return a > b ? a : b; }
 
@@ -92,12 +118,12 @@ template <bool Falling, int N, int O, typename V> __device__ __forceinline__ V s
 }
 template <typename V, bool Falling> __device__ __forceinline__ V sort64(V v) { return sort_steps<Falling, 2, 1>(v); }
 // The 64 best of a falling list and of 64 entries in any order.
-__device__ __forceinline__ uint64_t add64(uint64_t list, uint64_t more) {
-  return merge_falling(larger(list, sort64<uint64_t, false>(more)));
+template <typename V> __device__ __forceinline__ V add64(V list, V more) {
+  return merge_falling(larger(list, sort64<V, false>(more)));
 }
 
 // The waves' lists into one, in wave 0.  lds [kWaves][64].
-__device__ __forceinline__ uint64_t join_lists(uint64_t list, uint64_t (*lds)[64]) {
+template <typename V> __device__ __forceinline__ V join_lists(V list, V (*lds)[64]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   lds[wave][lane] = list;
   __syncthreads();
@@ -199,19 +225,21 @@ template <int DT, bool Top, bool Once>
 __global__ __launch_bounds__(kBlock, 5) void logprob_spans(const Fwd a) {
   constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
   __shared__ float s_sum[kWaves][3];
-  __shared__ uint64_t s_list[kWaves][Top ? 64 + 64 * E : 64];   // each wave's candidates: less than 64 and a vector's; its list at the end
+  using Entry = typename Local<DT>::type;
+  __shared__ Entry s_list[kWaves][Top ? 128 : 64];         // each wave's candidates: less than 64, and 64; its list at the end
   const int64_t row = blockIdx.x / (unsigned)a.spans;
   const int span = (int)(blockIdx.x % (unsigned)a.spans);
   const char* x = a.x + row * a.stride * EB;
   const int begin = span * a.span, end = min(a.vocab, begin + a.span);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Sum sum = {-kInf, 0.f, 0.f};
-  uint64_t list = 0;
+  Entry list = 0;
   float cut = -kInf;                                       // scores up to it are not among the k best
   int waiting = 0;
-  uint64_t* buf = s_list[wave];
-  // The next piece is requested ahead (with the lists beside it that costs more waves than it gains: 58 us for 55).
-  constexpr bool Ahead = !Top;
+  Entry* buf = s_list[wave];
+  // The next piece is requested ahead, but for 16-bit scores with lists, where it costs more waves than it gains (319 x 209950: 55 us
+  // for 52; float32, 622 x 107750: 71 for 77).
+  constexpr bool Ahead = !Top || DT == DMT_F32;
   dmt::Raw<DT, E> r[kVecs], next[kVecs];
   if (Ahead) load_piece<DT, Once>(x, begin, end, next);
   for (int j = begin; j < end; j += piece_elems<DT>()) {
@@ -222,15 +250,13 @@ __global__ __launch_bounds__(kBlock, 5) void logprob_spans(const Fwd a) {
     } else {
       load_piece<DT, Once>(x, j, end, r);
     }
-    float most[kVecs], pm = -kInf;
+    float pm = -kInf;
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
       float e[E];
       dmt::unpack<DT, E>(r[v], e);
-      most[v] = e[0];
 #pragma unroll
-      for (int q = 1; q < E; ++q) most[v] = fmaxf(most[v], e[q]);
-      pm = fmaxf(pm, most[v]);
+      for (int q = 0; q < E; ++q) pm = fmaxf(pm, e[q]);
     }
     if (pm > sum.m) rescale(sum, pm);
     const float m = or_zero(sum.m), m2 = m * kLog2e;
@@ -261,47 +287,50 @@ __global__ __launch_bounds__(kBlock, 5) void logprob_spans(const Fwd a) {
           const float below = bound == 0.f ? -__uint_as_float(1u) : __uint_as_float(bound > 0.f ? u - 1 : u + 1);
           low = fmaxf(low, bound == -kInf ? bound : below);
         }
-        // (a real loop, the pieces handed down: the sort in it is hundreds of instructions)
-#pragma unroll 1
+        uint32_t found = 0;                                // which of the lane's scores are above it
+#pragma unroll
         for (int v = 0; v < kVecs; ++v) {
-          if (__any(most[0] > low)) {
-            float e[E];
-            dmt::unpack<DT, E>(r[0], e);
+          float e[E];
+          dmt::unpack<DT, E>(r[v], e);
 #pragma unroll
-            for (int q = 0; q < E; ++q) {
-              const uint64_t mask = __ballot(e[q] > low);
-              if (!mask) continue;
-              if (mask >> lane & 1)
-                buf[waiting + __popcll(mask & ((1ull << lane) - 1))] =
-                    entry(e[q], (uint32_t)(j + (v * kBlock + (int)threadIdx.x) * E + q));
-              waiting += __popcll(mask);
-            }
-            __builtin_amdgcn_wave_barrier();
+          for (int q = 0; q < E; ++q) found |= (uint32_t)(e[q] > low) << (v * E + q);
+        }
+        // one of each lane's at a time, the score read again (few lanes have one, fewer two: taking them from the registers, a
+        // ballot and a branch for each of those, was most of the kernel's instructions)
+        for (;;) {
+          const uint64_t mask = __ballot(found != 0);
+          if (found) {
+            const int slot = __builtin_ctz(found), at = (slot / E * kBlock + (int)threadIdx.x) * E + slot % E;
+            found &= found - 1;
+            buf[waiting + __popcll(mask & ((1ull << lane) - 1))] =
+                Local<DT>::make(dmt::load1<DT>(x + ((int64_t)j + at) * EB), j - begin + at);
           }
-#pragma unroll
-          for (int w = 0; w + 1 < kVecs; ++w) r[w] = r[w + 1], most[w] = most[w + 1];
-          // a full wave of them, or what there is after the first piece (for its bound) and the last
-          while (waiting >= 64 || (waiting > 0 && v == kVecs - 1 && (last || j == begin))) {
+          __builtin_amdgcn_wave_barrier();
+          waiting += __popcll(mask);
+          // a full wave of them goes into the list, or what there is after the first piece (for its bound) and the last
+          const bool end_of_piece = !mask && (last || j == begin);
+          if (waiting >= 64 || (end_of_piece && waiting > 0)) {
             const int from = max(0, waiting - 64);
-            const uint64_t e = from + lane < waiting ? buf[from + lane] : 0;
+            const Entry e = from + lane < waiting ? buf[from + lane] : 0;
             __builtin_amdgcn_wave_barrier();
             waiting = from;
             list = add64(list, e);
           }
+          if (!mask) break;
         }
         // later pieces hold later items only: a score has to beat the k-th
-        cut = fmaxf(cut, __shfl(entry_score(list), a.k - 1));
+        cut = fmaxf(cut, __shfl(Local<DT>::score(list), a.k - 1));
       }
     }
   }
   sum = join_sums(sum, s_sum);
-  if constexpr (Top) list = join_lists(list, (uint64_t(*)[64])s_list);
+  if constexpr (Top) list = join_lists(list, (Entry(*)[64])s_list);
   if (a.spans == 1) {
-    finish<DT>(a, row, sum, list);
+    finish<DT>(a, row, sum, Local<DT>::wide(list, begin));
   } else {
     const int64_t at = row * a.spans + span;
     if (threadIdx.x == 0) a.part[at] = make_float4(sum.m, sum.s, sum.t, 0.f);
-    if (Top && (int)threadIdx.x < a.k) a.lists[at * a.k + threadIdx.x] = list;
+    if (Top && (int)threadIdx.x < a.k) a.lists[at * a.k + threadIdx.x] = Local<DT>::wide(list, begin);
   }
 }
 
@@ -382,16 +411,23 @@ __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, 
   else grads([&](float v) { return fmaf(v, kLog2e, -m2); });
 }
 
-// A row is cut into spans of whole pieces while the blocks are fewer than fit the chip at once.
+// A row is cut into spans of whole pieces while the blocks are fewer than fit the chip at once: eight of a CU, with the lists four (512 x
+// 100003, k = 20: 41 us with 1024 blocks, 47 with 2048).  Short rows stay whole, which saves the second launch: up to two pieces with
+// lists, which take 2 us each, and four without, at a quarter of one.  And a row's lists stay below kMostEntries, which the second
+// launch sorts: 262144 scores, k = 50: 10 + 10 us in 32 spans, 7 + 17 in 64.
 struct Spans {
   int spans, span;
 };
-constexpr int64_t kFillBlocks = 2048;
+constexpr int64_t kFillBlocks = 2048, kFillTop = 1024, kLeastPieces = 4, kLeastTop = 2, kMostEntries = 2048;
 constexpr int64_t kCacheBytes = 256 << 20;
-Spans spans_of(int64_t rows, int64_t vocab, int64_t piece) {
-  const int64_t pieces = (vocab + piece - 1) / piece;
-  const int64_t want = std::min(pieces, std::max<int64_t>(1, (kFillBlocks + rows - 1) / std::max<int64_t>(rows, 1)));
-  const int64_t per = (pieces + want - 1) / want;
+Spans spans_of(int64_t rows, int64_t vocab, int64_t piece, int k, int64_t most) {
+  const int64_t pieces = (vocab + piece - 1) / piece, fill = k > 0 ? kFillTop : kFillBlocks;
+  int64_t want = std::min(pieces, (fill + rows - 1) / rows);
+  if (k > 0) want = std::min(want, kMostEntries / k);
+  int64_t per = (pieces + want - 1) / want;
+  if (k == 0) per = std::max(per, std::min(kLeastPieces, pieces));
+  else if (pieces <= kLeastTop) per = pieces;
+  per = std::min(per, most / piece);
   return {(int)((pieces + per - 1) / per), (int)(per * piece)};
 }
 
@@ -408,7 +444,8 @@ extern "C" size_t dmt_token_logprob_workspace_bytes(int64_t rows, int64_t vocab,
   if (rows < 0 || vocab < 1 || k < 0 || k > DMT_TOP_MAX || !fits(rows, vocab)) return 0;
   // the most that any type, and any fewer rows, can need
   const int64_t pieces = (vocab + piece_elems<DMT_F32>() - 1) / piece_elems<DMT_F32>();
-  return part_bytes(std::min(rows * pieces, kFillBlocks + rows), k);
+  const int64_t least = (vocab + Local<DMT_BF16>::kMost - 1) / Local<DMT_BF16>::kMost;
+  return part_bytes(std::min(rows * pieces, kFillBlocks + rows * least), k);
 }
 
 extern "C" dmt_status dmt_token_logprob_fwd(const void* x, int64_t rows, int64_t vocab, int64_t x_stride,
@@ -423,8 +460,8 @@ extern "C" dmt_status dmt_token_logprob_fwd(const void* x, int64_t rows, int64_t
   if (rows > 0 && (!dmt_is_at(x, dmt_ebytes(dtype)) || (logprob && !targets) || (k > 0 && !top_ids))) return DMT_EINVAL;
   if (!fits(rows, vocab)) return DMT_ENOTSUP;
   const int64_t piece = dtype == DMT_F32 ? piece_elems<DMT_F32>() : piece_elems<DMT_BF16>();
-  const Spans sp = spans_of(rows, vocab, piece);
   if (rows == 0) return DMT_OK;
+  const Spans sp = spans_of(rows, vocab, piece, k, k > 0 && dtype != DMT_F32 ? Local<DMT_BF16>::kMost : 1 << 30);
   if (rows * sp.spans >= (1ll << 31)) return DMT_ENOTSUP;
   if (sp.spans > 1) {
     if (!dmt_is_at(workspace, 256)) return DMT_EINVAL;
