@@ -4,8 +4,11 @@
 // Forward, one pass over the scores.  A block takes a span of a row, 8 KB at a time in registers; every lane keeps a maximum, S
 // and T of its own and rescales them when its maximum grows.  Exponents are kept to the base 2: z = x log2 e - M log2 e is one
 // fused multiply-add, and M's product is rounded once and the same in every term (and in the backward), so its error cancels.
-// The top k: each wave holds its 64 best so far, sorted, one a lane.  The k-th largest of the lanes' maxima of a piece is a
-// bound that at least k scores reach, so only the few scores above it (and above the list's k-th) are looked at singly.
+// The top k: each wave holds its 64 best so far, sorted, one a lane, and looks singly at few scores only, those above a bound that at
+// least k scores reach.  The bound is the k-th largest of 64 maxima, the columns of all waves' running maxima, taken after pieces
+// 1, 2, 4, 8 ... of a span: of 13 pieces and k = 20 some 25 scores of a wave are looked at, where each wave's own k-th best let 75 through
+// (512 x 100003 float16: 34.8 us for 41.1, 2.9 TB/s; 622 x 107750 float32, k = 1: 52 for 71).  What is left is mostly arithmetic: the
+// sums of 16-bit scores take some 16 of the 35 us.
 // Rows are cut into spans when they are too few to fill the chip; a second launch joins the spans.
 #include <algorithm>
 #include <type_traits>
@@ -23,6 +26,12 @@ constexpr float kFar = 1e30f;                              // |M| beyond which M
 constexpr float kNone = -200.f;                            // 2^kNone is 0: stands for exponents down to -inf
 
 template <int DT> constexpr int piece_elems() { return kBlock * kVecs * dmt::ChunkElems<DT>::value; }
+
+// The largest float below x (x itself, where that is -inf).
+__device__ __forceinline__ float just_below(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return x == -kInf ? x : x == 0.f ? -__uint_as_float(1u) : __uint_as_float(x > 0.f ? u - 1 : u + 1);
+}
 
 // (x - m) log2 e;  m is not -inf.
 __device__ __forceinline__ float exponent(float x, float m) {
@@ -222,11 +231,12 @@ __device__ __forceinline__ void load_piece(const char* row, int j, int end, dmt:
 
 // Once: the scores pass the caches by.
 template <int DT, bool Top, bool Once>
-__global__ __launch_bounds__(kBlock, 5) void logprob_spans(const Fwd a) {
+__global__ __launch_bounds__(kBlock, Top ? 4 : 5) void logprob_spans(const Fwd a) {
   constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
   __shared__ float s_sum[kWaves][3];
   using Entry = typename Local<DT>::type;
-  __shared__ Entry s_list[kWaves][Top ? 128 : 64];         // each wave's candidates: less than 64, and 64; its list at the end
+  __shared__ Entry s_list[Top ? kWaves : 1][64];
+  __shared__ int s_buf[Top ? kWaves : 1][128];             // each wave's candidates, by their distance from `begin`: less than 64, and 64
   const int64_t row = blockIdx.x / (unsigned)a.spans;
   const int span = (int)(blockIdx.x % (unsigned)a.spans);
   const char* x = a.x + row * a.stride * EB;
@@ -236,20 +246,17 @@ __global__ __launch_bounds__(kBlock, 5) void logprob_spans(const Fwd a) {
   Entry list = 0;
   float cut = -kInf;                                       // scores up to it are not among the k best
   int waiting = 0;
-  Entry* buf = s_list[wave];
-  // The next piece is requested ahead, but for 16-bit scores with lists, where it costs more waves than it gains (319 x 209950: 55 us
-  // for 52; float32, 622 x 107750: 71 for 77).
-  constexpr bool Ahead = !Top || DT == DMT_F32;
+  int* buf = s_buf[Top ? wave : 0];
+  __shared__ float s_best[Top ? 2 : 1][kWaves][64];        // the lanes' maxima; two sets by turns, so that one barrier does
+  const bool shared = end - begin > piece_elems<DT>();      // (one piece: each wave by itself, 6.1 us for 6.5)
+  int piece = 0;
+  // the next piece is requested ahead (without: 319 x 209950 float16, k = 5: 43.9 us for 41.8; 512 x 100003, k = 20: 35.6 for 34.8)
   dmt::Raw<DT, E> r[kVecs], next[kVecs];
-  if (Ahead) load_piece<DT, Once>(x, begin, end, next);
+  load_piece<DT, Once>(x, begin, end, next);
   for (int j = begin; j < end; j += piece_elems<DT>()) {
-    if constexpr (Ahead) {
 #pragma unroll
-      for (int v = 0; v < kVecs; ++v) r[v] = next[v];
-      if (j + piece_elems<DT>() < end) load_piece<DT, Once>(x, j + piece_elems<DT>(), end, next);
-    } else {
-      load_piece<DT, Once>(x, j, end, r);
-    }
+    for (int v = 0; v < kVecs; ++v) r[v] = next[v];
+    if (j + piece_elems<DT>() < end) load_piece<DT, Once>(x, j + piece_elems<DT>(), end, next);
     float pm = -kInf;
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
@@ -276,17 +283,25 @@ __global__ __launch_bounds__(kBlock, 5) void logprob_spans(const Fwd a) {
     if (__any(fabsf(m) > kFar)) add([&](float v) { return exponent(v, m); });
     else add([&](float v) { return fmaf(v, kLog2e, -m2); });
     if constexpr (Top) {
-      const uint64_t over = __ballot(pm > cut);
       const bool last = j + piece_elems<DT>() >= end;
+      float low = cut;                                     // of this piece, candidates are above it
+      if (shared && (piece & (piece + 1)) == 0) {
+        // after pieces 1, 2, 4, 8 ...: at least k scores of the span so far reach the k-th largest of 64 maxima, each of a lane of
+        // every wave; in this piece equal ones may have lower items
+        float(*best)[64] = s_best[__popc((uint32_t)piece) & 1];
+        best[wave][lane] = sum.m;
+        __syncthreads();
+        float of = best[0][lane];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) of = fmaxf(of, best[w][lane]);
+        const float bound = __shfl(sort64<float, true>(of), a.k - 1);
+        low = fmaxf(low, just_below(bound));
+        cut = fmaxf(cut, bound);
+      }
+      ++piece;
+      const uint64_t over = __ballot(pm > low);
       if (over || (last && waiting > 0)) {
-        float low = cut;                                   // of this piece, candidates are above it
-        if (__popcll(over) >= a.k) {
-          // at least k scores reach the k-th largest of the lanes' maxima; equal ones may have lower items
-          const float bound = __shfl(sort64<float, true>(pm), a.k - 1);
-          const uint32_t u = __float_as_uint(bound);
-          const float below = bound == 0.f ? -__uint_as_float(1u) : __uint_as_float(bound > 0.f ? u - 1 : u + 1);
-          low = fmaxf(low, bound == -kInf ? bound : below);
-        }
+        if (__popcll(over) >= a.k) low = fmaxf(low, just_below(__shfl(sort64<float, true>(pm), a.k - 1)));
         uint32_t found = 0;                                // which of the lane's scores are above it
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
@@ -295,23 +310,22 @@ __global__ __launch_bounds__(kBlock, 5) void logprob_spans(const Fwd a) {
 #pragma unroll
           for (int q = 0; q < E; ++q) found |= (uint32_t)(e[q] > low) << (v * E + q);
         }
-        // one of each lane's at a time, the score read again (few lanes have one, fewer two: taking them from the registers, a
-        // ballot and a branch for each of those, was most of the kernel's instructions)
+        // one of each lane's at a time (few lanes have one, fewer two: taking them from the registers, a ballot and a branch for
+        // each of those, was most of the kernel's instructions); the scores are read again when they go into the list
         for (;;) {
           const uint64_t mask = __ballot(found != 0);
           if (found) {
-            const int slot = __builtin_ctz(found), at = (slot / E * kBlock + (int)threadIdx.x) * E + slot % E;
+            const int slot = __builtin_ctz(found);
             found &= found - 1;
-            buf[waiting + __popcll(mask & ((1ull << lane) - 1))] =
-                Local<DT>::make(dmt::load1<DT>(x + ((int64_t)j + at) * EB), j - begin + at);
+            buf[waiting + __popcll(mask & ((1ull << lane) - 1))] = j - begin + (slot / E * kBlock + (int)threadIdx.x) * E + slot % E;
           }
           __builtin_amdgcn_wave_barrier();
           waiting += __popcll(mask);
-          // a full wave of them goes into the list, or what there is after the first piece (for its bound) and the last
-          const bool end_of_piece = !mask && (last || j == begin);
-          if (waiting >= 64 || (end_of_piece && waiting > 0)) {
+          // a full wave of them goes into the list, or what there is after the last piece
+          if (waiting >= 64 || (!mask && last && waiting > 0)) {
             const int from = max(0, waiting - 64);
-            const Entry e = from + lane < waiting ? buf[from + lane] : 0;
+            const int at = buf[min(from + lane, 127)];
+            const Entry e = from + lane < waiting ? Local<DT>::make(dmt::load1<DT>(x + ((int64_t)begin + at) * EB), at) : 0;
             __builtin_amdgcn_wave_barrier();
             waiting = from;
             list = add64(list, e);
@@ -324,7 +338,7 @@ __global__ __launch_bounds__(kBlock, 5) void logprob_spans(const Fwd a) {
     }
   }
   sum = join_sums(sum, s_sum);
-  if constexpr (Top) list = join_lists(list, (Entry(*)[64])s_list);
+  if constexpr (Top) list = join_lists(list, s_list);
   if (a.spans == 1) {
     finish<DT>(a, row, sum, Local<DT>::wide(list, begin));
   } else {
@@ -411,10 +425,11 @@ __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, 
   else grads([&](float v) { return fmaf(v, kLog2e, -m2); });
 }
 
-// A row is cut into spans of whole pieces while the blocks are fewer than fit the chip at once: eight of a CU, with the lists four (512 x
-// 100003, k = 20: 41 us with 1024 blocks, 47 with 2048).  Short rows stay whole, which saves the second launch: up to two pieces with
-// lists, which take 2 us each, and four without, at a quarter of one.  And a row's lists stay below kMostEntries, which the second
-// launch sorts: 262144 scores, k = 50: 10 + 10 us in 32 spans, 7 + 17 in 64.
+// A row is cut into equal spans of whole pieces while the blocks are fewer than fit the chip at once: eight of a CU, with the lists four
+// (512 x 100003, k = 20: 35 us with 1024 blocks, 40 with 2048), and then as near to that as whole spans come (1003 x 12000, k = 20: 14.9 us
+// in one span each, 18.2 + 5.3 in two).  Short rows stay whole, which saves the second launch: up to two pieces with lists, which take
+// 2 us each, and four without, at a quarter of one.  And a row's lists stay below kMostEntries, which the second launch sorts:
+// 262144 scores, k = 50: 10 + 10 us in 32 spans, 7 + 17 in 64.
 struct Spans {
   int spans, span;
 };
@@ -422,13 +437,14 @@ constexpr int64_t kFillBlocks = 2048, kFillTop = 1024, kLeastPieces = 4, kLeastT
 constexpr int64_t kCacheBytes = 256 << 20;
 Spans spans_of(int64_t rows, int64_t vocab, int64_t piece, int k, int64_t most) {
   const int64_t pieces = (vocab + piece - 1) / piece, fill = k > 0 ? kFillTop : kFillBlocks;
-  int64_t want = std::min(pieces, (fill + rows - 1) / rows);
+  int64_t want = std::min(pieces, k > 0 ? std::max<int64_t>(1, (fill + rows / 2) / rows) : (fill + rows - 1) / rows);
   if (k > 0) want = std::min(want, kMostEntries / k);
   int64_t per = (pieces + want - 1) / want;
   if (k == 0) per = std::max(per, std::min(kLeastPieces, pieces));
   else if (pieces <= kLeastTop) per = pieces;
   per = std::min(per, most / piece);
-  return {(int)((pieces + per - 1) / per), (int)(per * piece)};
+  const int64_t spans = (pieces + per - 1) / per;
+  return {(int)spans, (int)((pieces + spans - 1) / spans * piece)};
 }
 
 // Sums and lists of so many spans.

@@ -414,6 +414,53 @@ def test_token_logprob_of_awkward_rows(dmt, vocab, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("copies,vocab", [(90, 9001), (150, 33_003), (47, 70_001)])
+def test_token_logprob_of_many_awkward_rows(dmt, copies, vocab, dt):
+    """As many rows as let a block walk through several thousand scores of one: ties, sorted rows, scores that all hide in one
+    wave's part, few scores that are left, the best ones in front or at the end."""
+    rng = np.random.default_rng(vocab + copies)
+    low = float(torch.finfo(DT[dt]).min)
+    at = np.arange(vocab)
+    x = np.full((12, vocab), -np.inf)
+    x[0] = 1.0
+    x[1] = at * (20.0 / vocab)
+    x[2] = -x[1]
+    x[3] = rng.integers(0, 4, vocab)
+    x[4] = np.where(at // 512 % 4 == 1, rng.normal(size=vocab), -9.0)
+    x[5, rng.choice(vocab, 30, False)] = rng.normal(size=30)
+    x[6] = low
+    x[6, ::97] = rng.normal(size=len(x[6, ::97]))
+    x[7] = np.where(at % 2 == 0, 0.0, -0.0)
+    x[7, vocab - 9:] = 3.0
+    x[8] = np.where(at < 40, 7.0, rng.normal(size=vocab))
+    x[9] = np.where(at % 64 == 5, rng.normal(size=vocab) + 4, rng.normal(size=vocab))
+    x[10] = rng.normal(size=vocab)
+    x = torch.from_numpy(x).to(DT[dt])
+    big = x.cuda().repeat(copies, 1)
+    rows = big.shape[0]
+    t = rng.integers(0, vocab, 12)
+    td = torch.from_numpy(np.tile(t, copies).astype(np.int32)).cuda()
+    x64 = f64(x)
+    far = np.where(np.isfinite(x64), np.abs(x64), 0).max(1)
+    tol = SUM + 8 * U32 * (2 + far)
+    over = lambda v: np.where(np.isneginf(v.astype(np.float32)), -np.inf, v)
+    for k in (1, 7, 20, 64):
+        with np.errstate(invalid="ignore", over="ignore"):
+            lp, h, ids, lps = sq.token_logprob(x64, t, k)
+        logprob, entropy, top_lp = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, k, device="cuda")
+        top = torch.full((rows, k), 77, dtype=torch.int32, device="cuda")
+        ws = bytes_buf(dmt.dmt_token_logprob_workspace_bytes(rows, vocab, k))
+        dmt.dmt_token_logprob_fwd(big, td, logprob, entropy, top, top_lp, None, ws)
+        with np.errstate(invalid="ignore", over="ignore"):
+            for c in range(copies):
+                mine = slice(12 * c, 12 * c + 12)
+                assert (top[mine].cpu().numpy() == ids).all(), (c, k)
+                close(logprob[mine], over(lp), np.where(np.isfinite(lp), tol + 4 * U32 * np.abs(lp), 0), "logprob")
+                close(entropy[mine], h, 2 * SUM * (1 + np.abs(h)) + 8 * U32 * 64, "entropy")
+                close(f64(top_lp[mine]), over(lps), tol[:, None] + 4 * U32 * np.abs(lps), "top log probabilities")
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("vocab", [5, 300, 20_000])
 def test_token_logprob_of_rows_that_are_not_finite(dmt, vocab, dt):
     rng = np.random.default_rng(vocab)
