@@ -604,7 +604,8 @@ dmt_status dmt_token_logprob_bwd(const void* x, int64_t rows, int64_t vocab, int
  *            (numel 0: data may be NULL); `out` dev of the same type and size, data itself
  *            (in place) or memory that overlaps no gradient; ignored by dmt_grad_norm
  *   norm     dev float32 [1] out; may be NULL for dmt_grad_clip
- * In place with c = 1 nothing is written.  DMT_ENOTSUP beyond 2^20 tensors or 2^40 elements in one.
+ * In place with c = 1 nothing is written.  DMT_ENOTSUP beyond 2^20 tensors, 2^40 elements in one or
+ * 2^44 in all.
  */
 typedef struct {
   const void* data;

@@ -1,9 +1,15 @@
 // dmt_embed_fwd, dmt_embed_bwd: a table's rows by id, scaled, and the table's gradient in dense form.
 //
+// Forward: out[i] = s W[id_i], in float32, rounded once.  Backward: dW[v] = s sum over id_i = v of g[i], ascending i; zeros (or
+// what was there) for rows that no id names.
+//
 // Backward.  The lookups are sorted by id, stably, as (id, position) records: few of them in one launch, many by a
 // radix sort of up to 11 bits a digit, three launches a digit.  Then equal tiles of the sorted records are walked, each
-// gradient row read once, and rows whose run spans tiles are joined from partial sums in a last launch.  One
+// gradient row read once, and rows whose run spans tiles are joined from partial sums in a last launch.  Up to a few
+// thousand ids one launch does it all: every block orders the ids of its own range of rows, sums them and clears the others.  One
 // writer per row, no atomics on values, every order fixed: the same bits every time.
+// 163840 ids, 1 M rows of 512 bytes (590 MB to move): 128 us, of which the order 35, the sums 53, the join 43, both with the
+// clearing beside them.  1003 ids, 10007 x 100: 10 us, a chain of latencies.
 #include <algorithm>
 #include <type_traits>
 
@@ -16,7 +22,8 @@ constexpr int kBlock = 256;
 
 // ------------------------------------------------------------------ forward
 
-// A group of 2^log2_lpr lanes per id; a lane takes 16 bytes of the table's row at a time.
+// A group of 2^log2_lpr lanes per id; a lane takes 16 bytes of the table's row at a time.  Bound by the rows' bytes out and what of the
+// table is not in a cache: 262144 ids, rows of 256 bytes, Zipf: 16.9 us, 67 MB written at 4 TB/s beside the reads; one id 1.6 us.
 template <int TD, int OD>
 __global__ __launch_bounds__(kBlock) void embed_fwd_kernel(
     const char* __restrict__ table, int64_t rows, int cols, int64_t table_stride,
@@ -117,7 +124,7 @@ __global__ __launch_bounds__(kSortBlock) void embed_digits(
 }
 
 // counts[block][digit] -> records of that digit in earlier blocks; totals[digit].  A wave per 64 digits and sixteenth of the
-// blocks (one thread per digit over all the blocks was a chain of dependent batches: 9.6 us at 160 blocks, now 3.5).
+// blocks (one thread per digit over all the blocks was a chain of dependent batches: 9.6 us at 160 blocks, now 5.1).
 constexpr int kStartsSegs = 16, kStartsBatch = 16;
 __global__ __launch_bounds__(64 * kStartsSegs) void embed_digit_starts(uint32_t* __restrict__ counts, int64_t nblk,
                                                                        int nd, uint32_t* __restrict__ totals) {
