@@ -286,6 +286,18 @@ def test_layer_norm_bwd(dmt, rows, cols, dt, gd, wd):
         assert torch.equal(dx, dy) and torch.equal(dg, dg2) and torch.equal(db, db2)
 
 
+MANY = [(513, 5), (5000, 17), (900, 33), (2100, 60), (800, 127), (2000, 130), (600, 200), (520, 511), (600, 1052), (513, 2049), (514, 4100),
+        (700, 8192), (520, 9001)]
+
+
+@pytest.mark.parametrize("dt,gd,wd", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("f16", "f32", "f16")])
+@pytest.mark.parametrize("rows,cols", MANY)
+def test_layer_norm_of_many_rows(dmt, rows, cols, dt, gd, wd):
+    """More rows than one launch of the backward takes, at every number of lanes a row."""
+    test_layer_norm_fwd(dmt, rows, cols, dt, wd)
+    test_layer_norm_bwd(dmt, rows, cols, dt, gd, wd)
+
+
 def test_layer_norm_gradients_against_differences(dmt):
     """Directional differences of the forward, computed in float64, against the kernel's gradients."""
     rng = np.random.default_rng(3)
