@@ -25,7 +25,8 @@ constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 constexpr float kFar = 1e30f;                              // |M| beyond which M log2 e may overflow
 constexpr float kNone = -200.f;                            // 2^kNone is 0: stands for exponents down to -inf
 
-template <int DT> constexpr int piece_elems() { return kBlock * kVecs * dmt::ChunkElems<DT>::value; }
+// of W waves
+template <int DT, int W = kWaves> constexpr int piece_elems() { return W * 64 * kVecs * dmt::ChunkElems<DT>::value; }
 
 // The largest float below x (x itself, where that is -inf).
 __device__ __forceinline__ float just_below(float x) {
@@ -141,11 +142,16 @@ template <typename V> __device__ __forceinline__ V join_lists(V list, V (*lds)[6
   return list;
 }
 
-// The threads' sums into one, the same in every thread.  Ends with a barrier.
-__device__ __forceinline__ Sum join_sums(Sum a, float (*lds)[3]) {
+// A wave's sums into one, the same in every lane.
+__device__ __forceinline__ Sum join_lanes(Sum a) {
   rescale(a, dmt::group_max<64>(a.m));
   a.s = dmt::group_sum<64>(a.s);
   a.t = dmt::group_sum<64>(a.t);
+  return a;
+}
+// The block's threads' into one, the same in every thread.  Ends with a barrier.
+__device__ __forceinline__ Sum join_sums(Sum a, float (*lds)[3]) {
+  a = join_lanes(a);
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) lds[wave][0] = a.m, lds[wave][1] = a.s, lds[wave][2] = a.t;
   __syncthreads();
@@ -167,7 +173,7 @@ __device__ __forceinline__ Sum join_sums(Sum a, float (*lds)[3]) {
 
 struct Fwd {
   const char* x;
-  int64_t stride;
+  int64_t stride, rows;
   int vocab, k, spans, span;                               // span: elements, a multiple of the piece
   const int32_t* targets;
   float *logprob, *entropy, *stats;
@@ -178,13 +184,13 @@ struct Fwd {
   uint64_t* lists;                                         // [row][span][k]
 };
 
-// A row's answers from its sums (known to every thread) and its list (wave 0's).
+// A row's answers from its sums (known to every thread) and its list (its first wave's), by the threads `tid` from 0 on.
 template <int DT>
-__device__ __forceinline__ void finish(const Fwd& a, int64_t row, const Sum& all, uint64_t list) {
+__device__ __forceinline__ void finish(const Fwd& a, int64_t row, int tid, const Sum& all, uint64_t list) {
   constexpr int EB = dmt::EltBytes<DT>::value;
   const bool empty = all.s == 0.f;
   const float m = or_zero(all.m), ls = log2f(all.s);
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     const int32_t at = a.targets ? a.targets[row] : -1;
     if (at >= a.vocab && a.first_bad) atomicMin(a.first_bad, (unsigned long long)row);
     if (a.logprob)
@@ -194,30 +200,31 @@ __device__ __forceinline__ void finish(const Fwd& a, int64_t row, const Sum& all
     if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - all.t / all.s) * kLn2;
     if (a.stats) a.stats[2 * row] = all.m, a.stats[2 * row + 1] = all.s;
   }
-  if ((int)threadIdx.x < a.k) {
-    a.top_ids[row * a.k + threadIdx.x] = list ? (int32_t)entry_item(list) : -1;
-    if (a.top_logprobs) a.top_logprobs[row * a.k + threadIdx.x] = list ? log_prob(entry_score(list), m, ls) : -kInf;
+  if (tid < a.k) {
+    a.top_ids[row * a.k + tid] = list ? (int32_t)entry_item(list) : -1;
+    if (a.top_logprobs) a.top_logprobs[row * a.k + tid] = list ? log_prob(entry_score(list), m, ls) : -kInf;
   }
 }
 
-// 8 KB of a row from element j on, -inf behind `end`.
-template <int DT, bool Once = false>
+// A piece of a row (8 KB for a block) from element j on, -inf behind `end`.
+template <int DT, bool Once = false, int W = kWaves>
 __device__ __forceinline__ void load_piece(const char* row, int j, int end, dmt::Raw<DT, dmt::ChunkElems<DT>::value> (&r)[kVecs]) {
-  constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value, W = dmt::Raw<DT, E>::kWords;
+  constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value, kWords = dmt::Raw<DT, E>::kWords;
   constexpr uint32_t kMasked = DT == DMT_F32 ? 0xff800000u : DT == DMT_F16 ? 0xfc00fc00u : 0xff80ff80u;
-  if (j + piece_elems<DT>() <= end) {
+  const int tid = (int)threadIdx.x % (W * 64);
+  if (j + piece_elems<DT, W>() <= end) {
 #pragma unroll
     for (int v = 0; v < kVecs; ++v)
-      r[v] = dmt::load_raw<DT, E, Once>(row + ((int64_t)j + (v * kBlock + (int)threadIdx.x) * E) * EB, E);
+      r[v] = dmt::load_raw<DT, E, Once>(row + ((int64_t)j + (v * W * 64 + tid) * E) * EB, E);
     return;
   }
 #pragma unroll
   for (int v = 0; v < kVecs; ++v) {
-    const int at = j + (v * kBlock + (int)threadIdx.x) * E, valid = end - at;
+    const int at = j + (v * W * 64 + tid) * E, valid = end - at;
     if (valid > 0) r[v] = dmt::load_raw<DT, E>(row + (int64_t)at * EB, valid);
     if (valid < E) {
 #pragma unroll
-      for (int q = 0; q < W; ++q) {
+      for (int q = 0; q < kWords; ++q) {
         if constexpr (DT == DMT_F32) {
           if (q >= valid) r[v].w[q] = kMasked;
         } else {
@@ -229,34 +236,38 @@ __device__ __forceinline__ void load_piece(const char* row, int j, int end, dmt:
   }
 }
 
-// Once: the scores pass the caches by.
-template <int DT, bool Top, bool Once>
+// Once: the scores pass the caches by.  W: waves of a row; with one a block takes four whole rows, and nothing crosses waves.
+template <int DT, bool Top, bool Once, int W>
 __global__ __launch_bounds__(kBlock, Top ? 4 : 5) void logprob_spans(const Fwd a) {
   constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
   __shared__ float s_sum[kWaves][3];
   using Entry = typename Local<DT>::type;
   __shared__ Entry s_list[Top ? kWaves : 1][64];
   __shared__ int s_buf[Top ? kWaves : 1][128];             // each wave's candidates, by their distance from `begin`: less than 64, and 64
-  const int64_t row = blockIdx.x / (unsigned)a.spans;
-  const int span = (int)(blockIdx.x % (unsigned)a.spans);
+  constexpr int kPiece = piece_elems<DT, W>();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t row = W == 1 ? (int64_t)blockIdx.x * kWaves + wave : blockIdx.x / (unsigned)a.spans;
+  const int span = W == 1 ? 0 : (int)(blockIdx.x % (unsigned)a.spans);
+  if (W == 1 && row >= a.rows) return;
+  const int tid = (int)threadIdx.x % (W * 64);
   const char* x = a.x + row * a.stride * EB;
   const int begin = span * a.span, end = min(a.vocab, begin + a.span);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Sum sum = {-kInf, 0.f, 0.f};
   Entry list = 0;
   float cut = -kInf;                                       // scores up to it are not among the k best
   int waiting = 0;
   int* buf = s_buf[Top ? wave : 0];
   __shared__ float s_best[Top ? 2 : 1][kWaves][64];        // the lanes' maxima; two sets by turns, so that one barrier does
-  const bool shared = end - begin > piece_elems<DT>();      // (one piece: each wave by itself, 6.1 us for 6.5)
+  // (one piece: each wave by itself, 6.1 us for 6.5; but k = 50 8192 x 1000 48 for 38)
+  const bool shared = W == 1 || end - begin > kPiece || a.k > 32;
   int piece = 0;
   // the next piece is requested ahead (without: 319 x 209950 float16, k = 5: 43.9 us for 41.8; 512 x 100003, k = 20: 35.6 for 34.8)
   dmt::Raw<DT, E> r[kVecs], next[kVecs];
-  load_piece<DT, Once>(x, begin, end, next);
-  for (int j = begin; j < end; j += piece_elems<DT>()) {
+  load_piece<DT, Once, W>(x, begin, end, next);
+  for (int j = begin; j < end; j += kPiece) {
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) r[v] = next[v];
-    if (j + piece_elems<DT>() < end) load_piece<DT, Once>(x, j + piece_elems<DT>(), end, next);
+    if (j + kPiece < end) load_piece<DT, Once, W>(x, j + kPiece, end, next);
     float pm = -kInf;
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
@@ -283,17 +294,20 @@ __global__ __launch_bounds__(kBlock, Top ? 4 : 5) void logprob_spans(const Fwd a
     if (__any(fabsf(m) > kFar)) add([&](float v) { return exponent(v, m); });
     else add([&](float v) { return fmaf(v, kLog2e, -m2); });
     if constexpr (Top) {
-      const bool last = j + piece_elems<DT>() >= end;
+      const bool last = j + kPiece >= end;
       float low = cut;                                     // of this piece, candidates are above it
       if (shared && (piece & (piece + 1)) == 0) {
         // after pieces 1, 2, 4, 8 ...: at least k scores of the span so far reach the k-th largest of 64 maxima, each of a lane of
         // every wave; in this piece equal ones may have lower items
-        float(*best)[64] = s_best[__popc((uint32_t)piece) & 1];
-        best[wave][lane] = sum.m;
-        __syncthreads();
-        float of = best[0][lane];
+        float of = sum.m;
+        if constexpr (W > 1) {
+          float(*best)[64] = s_best[__popc((uint32_t)piece) & 1];
+          best[wave][lane] = sum.m;
+          __syncthreads();
+          of = best[0][lane];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) of = fmaxf(of, best[w][lane]);
+          for (int w = 1; w < kWaves; ++w) of = fmaxf(of, best[w][lane]);
+        }
         const float bound = __shfl(sort64<float, true>(of), a.k - 1);
         low = fmaxf(low, just_below(bound));
         cut = fmaxf(cut, bound);
@@ -317,7 +331,7 @@ __global__ __launch_bounds__(kBlock, Top ? 4 : 5) void logprob_spans(const Fwd a
           if (found) {
             const int slot = __builtin_ctz(found);
             found &= found - 1;
-            buf[waiting + __popcll(mask & ((1ull << lane) - 1))] = j - begin + (slot / E * kBlock + (int)threadIdx.x) * E + slot % E;
+            buf[waiting + __popcll(mask & ((1ull << lane) - 1))] = j - begin + (slot / E * W * 64 + tid) * E + slot % E;
           }
           __builtin_amdgcn_wave_barrier();
           waiting += __popcll(mask);
@@ -337,14 +351,18 @@ __global__ __launch_bounds__(kBlock, Top ? 4 : 5) void logprob_spans(const Fwd a
       }
     }
   }
-  sum = join_sums(sum, s_sum);
-  if constexpr (Top) list = join_lists(list, s_list);
-  if (a.spans == 1) {
-    finish<DT>(a, row, sum, Local<DT>::wide(list, begin));
+  if constexpr (W == 1) {
+    sum = join_lanes(sum);
+  } else {
+    sum = join_sums(sum, s_sum);
+    if constexpr (Top) list = join_lists(list, s_list);
+  }
+  if (W == 1 || a.spans == 1) {
+    finish<DT>(a, row, tid, sum, Local<DT>::wide(list, begin));
   } else {
     const int64_t at = row * a.spans + span;
-    if (threadIdx.x == 0) a.part[at] = make_float4(sum.m, sum.s, sum.t, 0.f);
-    if (Top && (int)threadIdx.x < a.k) a.lists[at * a.k + threadIdx.x] = Local<DT>::wide(list, begin);
+    if (tid == 0) a.part[at] = make_float4(sum.m, sum.s, sum.t, 0.f);
+    if (Top && tid < a.k) a.lists[at * a.k + tid] = Local<DT>::wide(list, begin);
   }
 }
 
@@ -375,7 +393,7 @@ __global__ __launch_bounds__(kBlock) void logprob_join(const Fwd a) {
     list = join_lists(list, s_list);
   }
   sum = join_sums(sum, s_sum);
-  finish<DT>(a, row, sum, list);
+  finish<DT>(a, row, (int)threadIdx.x, sum, list);
 }
 
 // ------------------------------------------------------------------ backward
@@ -448,6 +466,15 @@ Spans spans_of(int64_t rows, int64_t vocab, int64_t piece, int k, int64_t most) 
   return {(int)spans, (int)((pieces + spans - 1) / spans * piece)};
 }
 
+// Whole rows, a wave each: nothing to join across waves, but fewer loads of a row under way and coarser shares.  Rows of a wave's own piece, and
+// while there are waves for half the chip (lists) or all of it: 8192 x 1000 float32, k = 10 17.7 us for 36.7; 2500 x 4000, k = 10 13.9 for
+// 15.8, no lists 16.8 for 15.4; 8192 x 8000 bfloat16, k = 10 42.6 for 55.0, no lists 83.0 for 85.5 with the backward; lists of long rows: 9000 x
+// 30000 123 for 137, but 2500 x 30000 60 for 51; long rows without: 8192 x 65536 187 for 168.
+bool wave_a_row(int64_t rows, int64_t vocab, int64_t piece, int k) {
+  const int64_t pieces = rows >= 4096 ? (k > 0 ? 16 : 4) : rows >= 2048 && k > 0 ? 4 : 0;
+  return vocab <= std::max(piece / kWaves, pieces * piece);
+}
+
 // Sums and lists of so many spans.
 size_t part_bytes(int64_t spans, int k) {
   return dmt_align_up(sizeof(float4) * (size_t)spans, 256) + sizeof(uint64_t) * (size_t)spans * (size_t)k;
@@ -485,20 +512,26 @@ extern "C" dmt_status dmt_token_logprob_fwd(const void* x, int64_t rows, int64_t
     if (workspace_bytes < part_bytes(rows * sp.spans, k)) return DMT_ENOMEM;
   }
   Fwd a = {};
-  a.x = (const char*)x, a.stride = x_stride, a.vocab = (int)vocab, a.k = k, a.spans = sp.spans, a.span = sp.span;
+  a.x = (const char*)x, a.stride = x_stride, a.rows = rows, a.vocab = (int)vocab, a.k = k, a.spans = sp.spans, a.span = sp.span;
   a.targets = targets, a.logprob = logprob, a.entropy = entropy, a.stats = stats;
   a.top_ids = top_ids, a.top_logprobs = top_logprobs, a.first_bad = (unsigned long long*)first_bad;
   a.part = (float4*)workspace;
   a.lists = (uint64_t*)((char*)workspace + dmt_align_up(sizeof(float4) * (size_t)rows * sp.spans, 256));
-  auto go = [&](auto spans, auto join) {
-    hipLaunchKernelGGL(spans, dim3((unsigned)(rows * sp.spans)), dim3(kBlock), 0, (hipStream_t)stream, a);
+  const bool narrow = sp.spans == 1 && wave_a_row(rows, vocab, piece, k);
+  auto go = [&](auto spans, auto spans_narrow, auto join) {
+    if (narrow) hipLaunchKernelGGL(spans_narrow, dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kBlock), 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL(spans, dim3((unsigned)(rows * sp.spans)), dim3(kBlock), 0, (hipStream_t)stream, a);
     if (sp.spans > 1) hipLaunchKernelGGL(join, dim3((unsigned)rows), dim3(kBlock), 0, (hipStream_t)stream, a);
   };
   auto type = [&](auto top, auto once) {
     constexpr bool Top = decltype(top)::value, Once = decltype(once)::value;
-    if (dtype == DMT_F32) go(logprob_spans<DMT_F32, Top, Once>, logprob_join<DMT_F32, Top>);
-    else if (dtype == DMT_F16) go(logprob_spans<DMT_F16, Top, Once>, logprob_join<DMT_F16, Top>);
-    else go(logprob_spans<DMT_BF16, Top, Once>, logprob_join<DMT_BF16, Top>);
+    auto of = [&](auto dt) {
+      constexpr int DT = decltype(dt)::value;
+      go(logprob_spans<DT, Top, Once, kWaves>, logprob_spans<DT, Top, Once, 1>, logprob_join<DT, Top>);
+    };
+    if (dtype == DMT_F32) of(std::integral_constant<int, DMT_F32>());
+    else if (dtype == DMT_F16) of(std::integral_constant<int, DMT_F16>());
+    else of(std::integral_constant<int, DMT_BF16>());
   };
   // Scores that the Infinity Cache does not hold for the backward need not pass through it: 1 GiB, forward 239 -> 212 us (its
   // backward 348 -> 363); 64 MiB would be 17.0 for 17.0 and the backward 22.8 for 21.6.

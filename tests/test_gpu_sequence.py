@@ -473,6 +473,23 @@ def test_token_logprob_of_many_awkward_rows(dmt, copies, vocab, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("copies,vocab", [(175, 700), (171, 2049), (342, 1000), (343, 5003), (350, 17_001)])
+def test_token_logprob_of_very_many_awkward_rows(dmt, copies, vocab, dt):
+    """As many rows as are taken by a wave each."""
+    test_token_logprob_of_many_awkward_rows(dmt, copies, vocab, dt)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(4099, 64), (4099, 3001), (5, 511), (4097, 8190)])
+def test_token_logprob_of_very_many_rows_without_lists(dmt, rows, vocab, dt):
+    rng = np.random.default_rng(vocab + rows)
+    x = matrix(rng, rows, vocab, dt, 3, 1, scale=2.5)
+    t = rng.integers(0, vocab, rows)
+    t[rows // 2], t[rows - 1] = -1, vocab + 5
+    check_logprob(dmt, x, t, 0)
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("vocab", [5, 300, 20_000])
 def test_token_logprob_of_rows_that_are_not_finite(dmt, vocab, dt):
     rng = np.random.default_rng(vocab)
