@@ -593,6 +593,11 @@ def test_clip(dmt, count, shift):
         check_clip(dmt, grads_of(rng, sizes, kinds, shift, 0.1), max_norm)
 
 
+@pytest.mark.parametrize("count", [133, 134, 135, 187, 188, 189, 269, 377])
+def test_clip_of_as_many_as_a_launch_holds(dmt, count):
+    test_clip(dmt, count, 1)
+
+
 @pytest.mark.parametrize("n", [1, 7, 8, 9, 2047, 2048, 2049, 8192, 16_383, 16_384, 16_385, 32_767, 32_768, 32_769, 65_536,
                                65_537, 1_000_003, 9_000_001])
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
