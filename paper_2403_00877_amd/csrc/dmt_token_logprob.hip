@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kBlock, Top ? 4 : 5) void logprob_spans(const Fwd a
       ++piece;
       const uint64_t over = __ballot(pm > low);
       if (over || (last && waiting > 0)) {
-        if (__popcll(over) >= a.k) low = fmaxf(low, just_below(__shfl(sort64<float, true>(pm), a.k - 1)));
+        if (__popcll(over) >= max(a.k, 12)) low = fmaxf(low, just_below(__shfl(sort64<float, true>(pm), a.k - 1)));
         uint32_t found = 0;                                // which of the lane's scores are above it
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
@@ -446,13 +446,14 @@ __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, 
 
 // A row is cut into equal spans of whole pieces while the blocks are fewer than fit the chip at once: eight of a CU, with the lists four
 // (512 x 100003, k = 20: 35 us with 1024 blocks, 40 with 2048), and then as near to that as whole spans come (1003 x 12000, k = 20: 14.9 us
-// in one span each, 18.2 + 5.3 in two).  Short rows stay whole, which saves the second launch: up to two pieces with lists, which take
-// 2 us each, and four without, at a quarter of one.  And a row's lists stay below kMostEntries, which the second launch sorts:
+// in one span each, 18.2 + 5.3 in two).  Short rows stay whole, which saves the second launch, the time of some 4.5 pieces with lists (60 x
+// 12000 bfloat16, k = 20, 3 pieces: 8.9 us for 10.6; 400 x 12000 float32, 6 pieces, three spans: 12.6 for 16.7; 60 x 12000 float32, six spans:
+// 11.5 for 11.1), and up to four pieces without, at a quarter of one.  And a row's lists stay below kMostEntries, which the second launch sorts:
 // 262144 scores, k = 50: 10 + 10 us in 32 spans, 7 + 17 in 64.
 struct Spans {
   int spans, span;
 };
-constexpr int64_t kFillBlocks = 2048, kFillTop = 1024, kLeastPieces = 4, kLeastTop = 2, kMostEntries = 2048;
+constexpr int64_t kFillBlocks = 2048, kFillTop = 1024, kLeastPieces = 4, kMostEntries = 2048;
 constexpr int64_t kCacheBytes = 256 << 20;
 Spans spans_of(int64_t rows, int64_t vocab, int64_t piece, int k, int64_t most) {
   const int64_t pieces = (vocab + piece - 1) / piece, fill = k > 0 ? kFillTop : kFillBlocks;
@@ -460,7 +461,7 @@ Spans spans_of(int64_t rows, int64_t vocab, int64_t piece, int k, int64_t most) 
   if (k > 0) want = std::min(want, kMostEntries / k);
   int64_t per = (pieces + want - 1) / want;
   if (k == 0) per = std::max(per, std::min(kLeastPieces, pieces));
-  else if (pieces <= kLeastTop) per = pieces;
+  else if (2 * pieces * (want - 1) <= 9 * want) per = pieces;      // (what the spans save is less than 4.5 pieces' time)
   per = std::min(per, most / piece);
   const int64_t spans = (pieces + per - 1) / per;
   return {(int)spans, (int)((pieces + spans - 1) / spans * piece)};
