@@ -448,7 +448,8 @@ __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, 
 // (512 x 100003, k = 20: 35 us with 1024 blocks, 40 with 2048), and then as near to that as whole spans come (1003 x 12000, k = 20: 14.9 us
 // in one span each, 18.2 + 5.3 in two).  Short rows stay whole, which saves the second launch, the time of some 4.5 pieces with lists (60 x
 // 12000 bfloat16, k = 20, 3 pieces: 8.9 us for 10.6; 400 x 12000 float32, 6 pieces, three spans: 12.6 for 16.7; 60 x 12000 float32, six spans:
-// 11.5 for 11.1), and up to four pieces without, at a quarter of one.  And a row's lists stay below kMostEntries, which the second launch sorts:
+// 11.5 for 11.1) and of some 16 without (12000 float32: 7 us for 10; 60 x 30000 float32, 15 pieces: 7.7 for 10.0; 60 x 60000 bfloat16, 15:
+// 10.7 for 9.8; 400: 15.5 for 17.1).  And a row's lists stay below kMostEntries, which the second launch sorts:
 // 262144 scores, k = 50: 10 + 10 us in 32 spans, 7 + 17 in 64.
 struct Spans {
   int spans, span;
@@ -460,8 +461,8 @@ Spans spans_of(int64_t rows, int64_t vocab, int64_t piece, int k, int64_t most) 
   int64_t want = std::min(pieces, k > 0 ? std::max<int64_t>(1, (fill + rows / 2) / rows) : (fill + rows - 1) / rows);
   if (k > 0) want = std::min(want, kMostEntries / k);
   int64_t per = (pieces + want - 1) / want;
-  if (k == 0) per = std::max(per, std::min(kLeastPieces, pieces));
-  else if (2 * pieces * (want - 1) <= 9 * want) per = pieces;      // (what the spans save is less than 4.5 pieces' time)
+  if (2 * pieces * (want - 1) <= (k > 0 ? 9 : 32) * want) per = pieces;      // (the spans would save less than 4.5 pieces' time, or 16)
+  else if (k == 0) per = std::max(per, std::min(kLeastPieces, pieces));
   per = std::min(per, most / piece);
   const int64_t spans = (pieces + per - 1) / per;
   return {(int)spans, (int)((pieces + spans - 1) / spans * piece)};
