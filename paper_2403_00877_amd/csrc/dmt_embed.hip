@@ -8,7 +8,7 @@
 // gradient row read once, and rows whose run spans tiles are joined from partial sums in a last launch.  Up to a few
 // thousand ids one launch does it all: every block orders the ids of its own range of rows, sums them and clears the others.  One
 // writer per row, no atomics on values, every order fixed: the same bits every time.
-// 163840 ids, 1 M rows of 512 bytes (590 MB to move): 128 us, of which the order 35, the sums 53, the join 43, both with the
+// 163840 ids, 1 M rows of 512 bytes (590 MB to move): 126 us, of which the order 35, the sums 53, the join 41, both with the
 // clearing beside them.  1003 ids, 10007 x 100: 10 us, a chain of latencies.
 #include <algorithm>
 #include <type_traits>

@@ -2,7 +2,7 @@
 //
 // The tensors are cut into units and the blocks stride over them.  A block sums squares in float64; the scaling's blocks each
 // add the blocks' sums up again, in the same order, rather than wait for a launch that does.  Bound by memory: the
-// gradients are read, then read and written: 872 MB in 180 tensors 569 us, 4.6 TB/s; 3.5 MB in 16 tensors 9.8 us, two launches.  (The
+// gradients are read, then read and written: 872 MB in 180 tensors 574 us, 4.6 TB/s; 3.5 MB in 16 tensors 10 us, two launches.  (The
 // scaling backwards, from what was read last: no faster.)
 // The tensors' addresses travel as kernel arguments: nothing is copied to the device and a call may be captured.
 #include <algorithm>
