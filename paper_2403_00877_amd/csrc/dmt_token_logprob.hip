@@ -3,7 +3,9 @@
 //
 // Forward, one pass over the scores.  A block takes a span of a row, 8 KB at a time in registers; every lane keeps a maximum, S
 // and T of its own and rescales them when its maximum grows.  Exponents are kept to the base 2: z = x log2 e - M log2 e is one
-// fused multiply-add, and M's product is rounded once and the same in every term (and in the backward), so its error cancels.
+// fused multiply-add; M's product is rounded once and the same in every term (and in the backward), at most 1/16 from what it should
+// be, so its error cancels.  Beyond |M| = 2^20, where it would grow, z = (x - M) log2 e, and a sum that crosses that line is
+// brought to the other side's terms.
 // The top k: each wave holds its 64 best so far, sorted, one a lane, and looks singly at few scores only, those above a bound that at
 // least k scores reach.  The bound is the k-th largest of 64 maxima, the columns of all waves' running maxima, taken after pieces
 // 1, 2, 4, 8 ... of a span: of 13 pieces and k = 20 some 25 scores of a wave are looked at, where each wave's own k-th best let 75 through
@@ -22,7 +24,8 @@ constexpr int kBlock = 256, kWaves = kBlock / 64;
 constexpr int kVecs = 2;                                   // 16-byte pieces of a lane under way
 constexpr float kInf = __builtin_inff();
 constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
-constexpr float kFar = 1e30f;                              // |M| beyond which M log2 e may overflow
+constexpr float kFar = 0x1p20f;                            // |M| beyond which M log2 e is not rounded but taken after the difference
+constexpr float kApart = 1e30f;                            // distances beyond which exponents of 2 may overflow
 constexpr float kNone = -200.f;                            // 2^kNone is 0: stands for exponents down to -inf
 
 // of W waves
@@ -34,27 +37,27 @@ __device__ __forceinline__ float just_below(float x) {
   return x == -kInf ? x : x == 0.f ? -__uint_as_float(1u) : __uint_as_float(x > 0.f ? u - 1 : u + 1);
 }
 
-// (x - m) log2 e;  m is not -inf.
+// (x - m) log2 e + residue(m);  m is not -inf.
 __device__ __forceinline__ float exponent(float x, float m) {
   return fabsf(m) > kFar ? (x - m) * kLog2e : fmaf(x, kLog2e, -(m * kLog2e));
 }
+// What the rounding of m's product adds to every exponent, exactly; |residue| <= 1/16.
+__device__ __forceinline__ float residue(float m) { return fabsf(m) > kFar ? 0.f : fmaf(m, kLog2e, -(m * kLog2e)); }
 __device__ __forceinline__ float or_zero(float m) { return m == -kInf ? 0.f : m; }
 
 // log p of score x;  ls = log2 S.  (Far below M, exponents of 2 would overflow before natural ones do.)
 __device__ __forceinline__ float log_prob(float x, float m, float ls) {
-  return fabsf(x - m) > kFar ? x - m - ls * kLn2 : (exponent(x, m) - ls) * kLn2;
+  return fabsf(x - m) > kApart ? x - m - ls * kLn2 : (exponent(x, m) - ls) * kLn2;
 }
 
 struct Sum {
   float m, s, t;                                           // t in units of ln 2
 };
 
-// What `a` is with the maximum m (>= a.m).  Its terms hold a.m's rounded product, so that is what is taken back: equal
-// maxima leave the sums as they are.
+// What `a` is with the maximum m (>= a.m).  Its terms hold a.m's residue and get m's; equal maxima leave the sums as they are.
 __device__ __forceinline__ void rescale(Sum& a, float m) {
-#pragma clang fp contract(off)
-  const float far = (a.m - m) * kLog2e, near = a.m * kLog2e - m * kLog2e;
-  const float d = a.m == -kInf ? kNone : fabsf(m) > kFar ? far : near, f = __builtin_amdgcn_exp2f(d);
+  const float by = (a.m - m) * kLog2e + (residue(m) - residue(a.m));
+  const float d = a.m == -kInf ? kNone : by, f = __builtin_amdgcn_exp2f(d);
   a.t = f == 0.f ? 0.f : f * fmaf(d, a.s, a.t);
   a.s *= f;                                                // (a NaN stays)
   a.m = m;
