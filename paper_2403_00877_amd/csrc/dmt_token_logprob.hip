@@ -201,7 +201,7 @@ __device__ __forceinline__ void finish(const Fwd& a, int64_t row, int tid, const
                        : empty                 ? -kInf
                                                : log_prob(dmt::load1<DT>(a.x + (row * a.stride + at) * EB), m, ls);
     if (a.entropy) a.entropy[row] = empty ? 0.f : (ls - all.t / all.s) * kLn2;
-    if (a.stats) a.stats[2 * row] = all.m, a.stats[2 * row + 1] = all.s;
+    if (a.stats) a.stats[2 * row] = all.m, a.stats[2 * row + 1] = all.s * __builtin_amdgcn_exp2f(-residue(m));
   }
   if (tid < a.k) {
     a.top_ids[row * a.k + tid] = list ? (int32_t)entry_item(list) : -1;
@@ -401,8 +401,9 @@ __global__ __launch_bounds__(kBlock) void logprob_join(const Fwd a) {
 
 // ------------------------------------------------------------------ backward
 
-// dx = p (A + B z) with p = exp2(z) / S, z to the base 2:  A = -g_lp - g_H (H - log S),  B = -g_H ln 2.  A block takes a piece
-// of a row; bound by memory: 8192 x 65536 bfloat16 363 us, 5.9 TB/s, behind a forward of 210 (5.1, from past the caches).
+// dx = p (A + B z) with p = exp2(z) / S, z to the base 2:  A = -g_lp - g_H (H - log S),  B = -g_H ln 2, S with the residue that
+// the terms here have and the kept sum has not.  A block takes a piece of a row; bound by memory: 8192 x 65536 bfloat16 363 us,
+// 5.9 TB/s, behind a forward of 210 (5.1, from past the caches).
 template <int DT>
 __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, int64_t stride, int pieces,
                                                       const int32_t* __restrict__ targets,
@@ -418,7 +419,7 @@ __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, 
   char* dr = dx + row * dx_stride * EB;
   dmt::Raw<DT, E> r[kVecs];
   load_piece<DT>(xr, j, vocab, r);
-  const float m = or_zero(stats[2 * row]), s = stats[2 * row + 1], inv = s == 0.f ? 0.f : 1.f / s;
+  const float m = or_zero(stats[2 * row]), s = stats[2 * row + 1] * __builtin_amdgcn_exp2f(residue(m)), inv = s == 0.f ? 0.f : 1.f / s;
   const int32_t at = targets ? targets[row] : -1;
   const float gl = grad_logprob && at >= 0 && at < vocab ? grad_logprob[row] : 0.f;
   const float gh = grad_entropy ? grad_entropy[row] : 0.f, h = grad_entropy ? entropy[row] : 0.f;
