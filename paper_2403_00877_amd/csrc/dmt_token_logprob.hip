@@ -25,7 +25,7 @@ constexpr int kVecs = 2;                                   // 16-byte pieces of 
 constexpr float kInf = __builtin_inff();
 constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 constexpr float kFar = 0x1p20f;                            // |M| beyond which M log2 e is not rounded but taken after the difference
-constexpr float kApart = 1e30f;                            // distances beyond which exponents of 2 may overflow
+constexpr float kApart = 1e30f;                            // distances (and gradients) beyond which a few products may overflow
 constexpr float kNone = -200.f;                            // 2^kNone is 0: stands for exponents down to -inf
 
 // of W waves
@@ -422,9 +422,9 @@ __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, 
   const float m = or_zero(stats[2 * row]), s = stats[2 * row + 1] * __builtin_amdgcn_exp2f(residue(m)), inv = s == 0.f ? 0.f : 1.f / s;
   const int32_t at = targets ? targets[row] : -1;
   const float gl = grad_logprob && at >= 0 && at < vocab ? grad_logprob[row] : 0.f;
-  const float gh = grad_entropy ? grad_entropy[row] : 0.f, h = grad_entropy ? entropy[row] : 0.f;
+  const float gh = grad_entropy && s != 0.f ? grad_entropy[row] : 0.f, h = grad_entropy ? entropy[row] : 0.f;
   const float A = s == 0.f ? 0.f : (-gl - gh * (h - logf(s))) * inv, B = -gh * kLn2 * inv, m2 = m * kLog2e;
-  auto grads = [&](auto z) {
+  auto grads = [&](auto z, auto masks) {
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
       const int c = j + (v * kBlock + (int)threadIdx.x) * E;
@@ -435,6 +435,7 @@ __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, 
       for (int q = 0; q < E; ++q) {
         const float w = z(e[q]);
         d[q] = __builtin_amdgcn_exp2f(w) * fmaf(B, fmaxf(w, kNone), A);
+        if (decltype(masks)::value && e[q] == -kInf) d[q] = 0.f;
       }
       if (gl != 0.f && (uint32_t)(at - c) < (uint32_t)E) {
 #pragma unroll
@@ -444,8 +445,10 @@ __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, 
       dmt::store_elems<DT, E>(dr + (int64_t)c * EB, min(E, vocab - c), d);
     }
   };
-  if (fabsf(m) > kFar) grads([&](float v) { return exponent(v, m); });
-  else grads([&](float v) { return fmaf(v, kLog2e, -m2); });
+  // a masked score's exponential is 0, which is its gradient as long as the other factor is finite
+  if (!(fabsf(A) < kApart && fabsf(B) < kApart)) grads([&](float v) { return exponent(v, m); }, std::true_type());
+  else if (fabsf(m) > kFar) grads([&](float v) { return exponent(v, m); }, std::false_type());
+  else grads([&](float v) { return fmaf(v, kLog2e, -m2); }, std::false_type());
 }
 
 // A row is cut into equal spans of whole pieces while the blocks are fewer than fit the chip at once: eight of a CU, with the lists four
