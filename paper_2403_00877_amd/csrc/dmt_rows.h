@@ -206,3 +206,11 @@ static inline int64_t dmt_ebytes(int32_t t) { return t == DMT_F32 ? 4 : 2; }
 static inline bool dmt_is_at(const void* p, int64_t align) { return p && ((uintptr_t)p & (uintptr_t)(align - 1)) == 0; }
 // Whether an optional pointer is absent or aligned.
 static inline bool dmt_may_be_at(const void* p, int64_t align) { return ((uintptr_t)p & (uintptr_t)(align - 1)) == 0; }
+
+// Calls go(first block, grid) for the launches that `blocks` blocks of `threads` threads take: one is of fewer than 2^32 threads (the
+// runtime starts some of the blocks of a larger one, and reports nothing).
+template <typename Go> static inline void dmt_launches(int64_t blocks, int64_t threads, Go go) {
+  const int64_t most = ((1ll << 32) - 1) / threads;
+  for (int64_t first = 0; first < blocks; first += most)
+    go((unsigned)first, dim3((unsigned)(blocks - first < most ? blocks - first : most)));
+}

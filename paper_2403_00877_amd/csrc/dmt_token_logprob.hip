@@ -178,6 +178,7 @@ struct Fwd {
   const char* x;
   int64_t stride, rows;
   int vocab, k, spans, span;                               // span: elements, a multiple of the piece
+  unsigned first_block;                                    // of the launch, among the call's
   const int32_t* targets;
   float *logprob, *entropy, *stats;
   int32_t* top_ids;
@@ -249,8 +250,9 @@ __global__ __launch_bounds__(kBlock, Top ? 4 : 5) void logprob_spans(const Fwd a
   __shared__ int s_buf[Top ? kWaves : 1][128];             // each wave's candidates, by their distance from `begin`: less than 64, and 64
   constexpr int kPiece = piece_elems<DT, W>();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int64_t row = W == 1 ? (int64_t)blockIdx.x * kWaves + wave : blockIdx.x / (unsigned)a.spans;
-  const int span = W == 1 ? 0 : (int)(blockIdx.x % (unsigned)a.spans);
+  const unsigned block = a.first_block + blockIdx.x;
+  const int64_t row = W == 1 ? (int64_t)block * kWaves + wave : block / (unsigned)a.spans;
+  const int span = W == 1 ? 0 : (int)(block % (unsigned)a.spans);
   if (W == 1 && row >= a.rows) return;
   const int tid = (int)threadIdx.x % (W * 64);
   const char* x = a.x + row * a.stride * EB;
@@ -374,7 +376,7 @@ template <int DT, bool Top>
 __global__ __launch_bounds__(kBlock) void logprob_join(const Fwd a) {
   __shared__ float s_sum[kWaves][3];
   __shared__ uint64_t s_list[kWaves][64];
-  const int64_t row = blockIdx.x;
+  const int64_t row = a.first_block + blockIdx.x;
   Sum sum = {-kInf, 0.f, 0.f};
   for (int i = threadIdx.x; i < a.spans; i += kBlock) {
     const float4 p = a.part[row * a.spans + i];
@@ -405,7 +407,7 @@ __global__ __launch_bounds__(kBlock) void logprob_join(const Fwd a) {
 // the terms here have and the kept sum has not.  A block takes a piece of a row; bound by memory: 8192 x 65536 bfloat16 363 us,
 // 5.9 TB/s, behind a forward of 210 (5.1, from past the caches).
 template <int DT>
-__global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, int64_t stride, int pieces,
+__global__ __launch_bounds__(kBlock) void logprob_bwd(unsigned first_block, const char* x, int vocab, int64_t stride, int pieces,
                                                       const int32_t* __restrict__ targets,
                                                       const float* __restrict__ stats,
                                                       const float* __restrict__ entropy,
@@ -413,8 +415,9 @@ __global__ __launch_bounds__(kBlock) void logprob_bwd(const char* x, int vocab, 
                                                       const float* __restrict__ grad_entropy, char* dx,
                                                       int64_t dx_stride) {
   constexpr int E = dmt::ChunkElems<DT>::value, EB = dmt::EltBytes<DT>::value;
-  const int64_t row = blockIdx.x / (unsigned)pieces;
-  const int j = (int)(blockIdx.x % (unsigned)pieces) * piece_elems<DT>();
+  const unsigned block = first_block + blockIdx.x;
+  const int64_t row = block / (unsigned)pieces;
+  const int j = (int)(block % (unsigned)pieces) * piece_elems<DT>();
   const char* xr = x + row * stride * EB;
   char* dr = dx + row * dx_stride * EB;
   dmt::Raw<DT, E> r[kVecs];
@@ -527,10 +530,16 @@ extern "C" dmt_status dmt_token_logprob_fwd(const void* x, int64_t rows, int64_t
   a.part = (float4*)workspace;
   a.lists = (uint64_t*)((char*)workspace + dmt_align_up(sizeof(float4) * (size_t)rows * sp.spans, 256));
   const bool narrow = sp.spans == 1 && wave_a_row(rows, vocab, piece, k);
+  auto launch = [&](auto kernel, int64_t blocks) {
+    dmt_launches(blocks, kBlock, [&](unsigned first, dim3 grid) {
+      a.first_block = first;
+      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, (hipStream_t)stream, a);
+    });
+  };
   auto go = [&](auto spans, auto spans_narrow, auto join) {
-    if (narrow) hipLaunchKernelGGL(spans_narrow, dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kBlock), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL(spans, dim3((unsigned)(rows * sp.spans)), dim3(kBlock), 0, (hipStream_t)stream, a);
-    if (sp.spans > 1) hipLaunchKernelGGL(join, dim3((unsigned)rows), dim3(kBlock), 0, (hipStream_t)stream, a);
+    if (narrow) launch(spans_narrow, (rows + kWaves - 1) / kWaves);
+    else launch(spans, rows * sp.spans);
+    if (sp.spans > 1) launch(join, rows);
   };
   auto type = [&](auto top, auto once) {
     constexpr bool Top = decltype(top)::value, Once = decltype(once)::value;
@@ -571,8 +580,10 @@ extern "C" dmt_status dmt_token_logprob_bwd(const void* x, int64_t rows, int64_t
   const int64_t pieces = (vocab + piece - 1) / piece;
   if (rows * pieces >= (1ll << 31)) return DMT_ENOTSUP;
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * pieces)), dim3(kBlock), 0, (hipStream_t)stream, (const char*)x,
-                       (int)vocab, x_stride, (int)pieces, targets, stats, entropy, grad_logprob, grad_entropy, (char*)dx, dx_stride);
+    dmt_launches(rows * pieces, kBlock, [&](unsigned first, dim3 grid) {
+      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, (hipStream_t)stream, first, (const char*)x, (int)vocab, x_stride, (int)pieces,
+                         targets, stats, entropy, grad_logprob, grad_entropy, (char*)dx, dx_stride);
+    });
   };
   if (dtype == DMT_F32) go(logprob_bwd<DMT_F32>);
   else if (dtype == DMT_F16) go(logprob_bwd<DMT_F16>);
