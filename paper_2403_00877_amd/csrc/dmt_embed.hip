@@ -31,12 +31,12 @@ template <int E> __device__ __forceinline__ int piece_at(int c, int cols) { retu
 // table is not in a cache: 262144 ids, rows of 256 bytes, Zipf: 16.9 us, 67 MB written at 4 TB/s beside the reads; one id 1.6 us.
 template <int TD, int OD>
 __global__ __launch_bounds__(kBlock) void embed_fwd_kernel(
-    const char* __restrict__ table, int64_t rows, int cols, int64_t table_stride,
+    unsigned first_block, const char* __restrict__ table, int64_t rows, int cols, int64_t table_stride,
     const int32_t* __restrict__ ids, int64_t n, float scale, char* __restrict__ out, int64_t out_stride,
     unsigned long long* __restrict__ first_bad, int log2_lpr) {
   constexpr int E = dmt::ChunkElems<TD>::value, TB = dmt::EltBytes<TD>::value, OB = dmt::EltBytes<OD>::value;
   const int lane = threadIdx.x & ((1 << log2_lpr) - 1);
-  const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> log2_lpr;
+  const int64_t i = ((int64_t)(first_block + blockIdx.x) * kBlock + threadIdx.x) >> log2_lpr;
   if (i >= n) return;
   const int32_t id = ids[i];
   const bool there = id >= 0 && id < rows;
@@ -820,10 +820,11 @@ template <int TD>
 void launch_fwd(int32_t od, const void* table, int64_t rows, int64_t cols, int64_t ts, const int32_t* ids,
                 int64_t n, float scale, void* out, int64_t os, int64_t* bad, hipStream_t s) {
   const int l = log2_lanes(cols, dmt::ChunkElems<TD>::value);
-  const dim3 grid((unsigned)(((n << l) + kBlock - 1) / kBlock));
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, (const char*)table, rows, (int)cols, ts, ids, n, scale,
-                       (char*)out, os, (unsigned long long*)bad, l);
+    dmt_launches(((n << l) + kBlock - 1) / kBlock, kBlock, [&](unsigned first, dim3 grid) {
+      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, first, (const char*)table, rows, (int)cols, ts, ids, n, scale,
+                         (char*)out, os, (unsigned long long*)bad, l);
+    });
   };
   if (od == DMT_F32) go(embed_fwd_kernel<TD, DMT_F32>);
   else if (od == DMT_F16) go(embed_fwd_kernel<TD, DMT_F16>);

@@ -61,3 +61,22 @@ def test_token_logprob_of_more_rows_than_a_launch_holds(dmt):
         assert bool((st[a:b, 0] == best[:, 0]).all()), a
         want = gl[a:b, None].double() * (torch.zeros_like(p).scatter_(1, at, 1.0) - p)
         assert bool(((dx[a:b] - want).abs() <= UBF * want.abs() + 64 * U32).all()), a
+
+
+def test_embed_fwd_of_more_ids_than_a_launch_holds(dmt):
+    """2^26 ids and a few, a wave each."""
+    need(40)
+    n, rows, cols = (1 << 26) + 3, 1000, 129
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    table = torch.randn(rows, cols, generator=g, device="cuda")
+    ids = torch.randint(-1, rows, (n,), generator=g, device="cuda", dtype=torch.int32)
+    ids[n - 2] = rows
+    out = torch.full((n, cols), 7.0, dtype=torch.float16, device="cuda")
+    bad = torch.full((1,), -1, dtype=torch.int64, device="cuda")
+    dmt.dmt_embed_fwd(table, ids, out, first_bad=bad)
+    assert int(bad) == n - 2
+    there = torch.cat([table, torch.zeros(1, cols, device="cuda")]).half()      # row `rows`: of absent ids
+    for a in range(0, n, 1 << 24):
+        i = ids[a:a + (1 << 24)].long()
+        assert torch.equal(out[a:a + (1 << 24)], there[torch.where(i < 0, rows, i)]), a
