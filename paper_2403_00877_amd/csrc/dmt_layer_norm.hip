@@ -159,11 +159,11 @@ __global__ __launch_bounds__(T < kBlock ? kBlock : T) void norm_fwd(const Fwd a)
 
 // Rows of any length, a block each, read three times.
 template <int XD>
-__global__ __launch_bounds__(1024) void norm_fwd_long(const Fwd a) {
+__global__ __launch_bounds__(1024) void norm_fwd_long(const Fwd a, unsigned first_block) {
   constexpr int E = dmt::ChunkElems<XD>::value, XB = dmt::EltBytes<XD>::value, B = 1024;
   __shared__ float sm[2 * B / 64];
   int half = 0;
-  const int64_t r = blockIdx.x;
+  const int64_t r = first_block + blockIdx.x;
   const char* xr = a.x + r * a.x_stride * XB;
   float s[1] = {0.f}, x[E], w[E];
   for (int c = threadIdx.x * E; c < a.cols; c += B * E) {
@@ -386,11 +386,11 @@ __global__ __launch_bounds__(T < kBlock ? kBlock : T) void norm_bwd(const Bwd a)
 
 // Rows of any length: the rows' part and, a slice of the rows a block, the columns'.
 template <int XD, int GD>
-__global__ __launch_bounds__(1024) void norm_bwd_long(const Bwd a) {
+__global__ __launch_bounds__(1024) void norm_bwd_long(const Bwd a, unsigned first_block) {
   constexpr int E = dmt::ChunkElems<XD>::value, XB = dmt::EltBytes<XD>::value, GB = dmt::EltBytes<GD>::value, B = 1024;
   __shared__ float sm[2 * 2 * B / 64];
   int half = 0;
-  const int64_t r = blockIdx.x;
+  const int64_t r = first_block + blockIdx.x;
   const float m = a.mean[r], rs = a.rstd[r];
   float sums[2] = {0.f, 0.f}, h[E], d[E], w[E];
   for (int turn = 0; turn < 2; ++turn) {
@@ -540,7 +540,8 @@ extern "C" dmt_status dmt_layer_norm_fwd(const void* x, int64_t rows, int64_t co
       const int64_t blocks = std::min((rows + B / T - 1) / (B / T), fwd_blocks(T));
       hipLaunchKernelGGL((norm_fwd<XD, T, decltype(nv)::value>), dim3((unsigned)blocks), dim3(B), 0, s, a);
     });
-    if (!done) hipLaunchKernelGGL(norm_fwd_long<XD>, dim3((unsigned)rows), dim3(1024), 0, s, a);
+    if (!done)
+      dmt_launches(rows, 1024, [&](unsigned first, dim3 grid) { hipLaunchKernelGGL(norm_fwd_long<XD>, grid, dim3(1024), 0, s, a, first); });
   };
   if (dtype == DMT_F32) go(Int<DMT_F32>());
   else if (dtype == DMT_F16) go(Int<DMT_F16>());
@@ -577,7 +578,8 @@ static void bwd_run(Bwd a, hipStream_t s) {
     if (a.part)
       hipLaunchKernelGGL((norm_bwd_slices<XD, GD>), dim3((unsigned)((a.cols + kBlock - 1) / kBlock), (unsigned)parts), dim3(kBlock), 0,
                          s, a, per);
-    hipLaunchKernelGGL((norm_bwd_long<XD, GD>), dim3((unsigned)a.rows), dim3(1024), 0, s, a);
+    dmt_launches(a.rows, 1024,
+                 [&](unsigned first, dim3 grid) { hipLaunchKernelGGL((norm_bwd_long<XD, GD>), grid, dim3(1024), 0, s, a, first); });
   }
   if (a.part)
     hipLaunchKernelGGL(norm_bwd_sum, dim3((unsigned)((a.cols + 63) / 64), 2), dim3(1024), 0, s, a.part, parts, a.cols, a.dgamma, a.dbeta);
