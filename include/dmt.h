@@ -545,7 +545,8 @@ dmt_status dmt_layer_norm_fwd(const void* x, int64_t rows, int64_t cols, int64_t
  *   dx = rstd * (g - mean_c(g) - h * mean_c(g * h)),  dgamma = sum_rows dy * h,  dbeta = sum_rows dy
  *   dy, dx         [rows][cols] of grad_dtype (dtype or DMT_F32); dx may be dy itself (same stride)
  *   dgamma, dbeta  float32 [cols], overwritten; either may be NULL
- *   workspace      dmt_layer_norm_bwd_workspace_bytes(rows, cols); may be NULL when both are NULL
+ *   workspace      dmt_layer_norm_bwd_workspace_bytes(rows, cols); may be NULL when both are NULL, or when
+ *                  that is 0 (no rows: both are filled with zeros)
  */
 size_t dmt_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t cols);
 dmt_status dmt_layer_norm_bwd(const void* x, int64_t rows, int64_t cols, int64_t x_stride,

@@ -558,6 +558,7 @@ template <int XD, int GD>
 static void bwd_run(Bwd a, hipStream_t s) {
   const int64_t pieces = (a.cols + dmt::ChunkElems<XD>::value - 1) / dmt::ChunkElems<XD>::value;
   int64_t parts = 0;
+  bool sum = a.dgamma || a.dbeta;                           // whether partial sums are added up (no rows: none are, into zeros)
   const bool done = bwd_shape<dmt::ChunkElems<XD>::value>(pieces, [&](auto t, auto nv) {
     constexpr int T = decltype(t)::value, B = T < kBlock ? kBlock : T;
     parts = std::min((a.rows + B / T - 1) / (B / T), bwd_blocks(T));
@@ -565,8 +566,8 @@ static void bwd_run(Bwd a, hipStream_t s) {
       a.row_blocks = rows;
       if (rows + columns > 0) hipLaunchKernelGGL((norm_bwd<XD, GD, T, decltype(nv)::value>), dim3(rows + columns), dim3(B), 0, s, a);
     };
-    const unsigned columns = a.rows <= kFewRows && a.part ? (unsigned)((a.cols + 63) / 64) : 0u;
-    if (columns > 0) a.part = nullptr;
+    const unsigned columns = a.rows <= kFewRows && sum ? (unsigned)((a.cols + 63) / 64) : 0u;
+    if (columns > 0) a.part = nullptr, sum = false;
     const bool ahead = (const char*)a.dx == a.dy || (const char*)a.dx == a.x;      // dx in the place of what the columns read
     if (columns > 0 && ahead) launch(0, columns);
     launch((unsigned)parts, ahead ? 0 : columns);
@@ -575,13 +576,13 @@ static void bwd_run(Bwd a, hipStream_t s) {
     const int64_t per = (a.rows + kSlices - 1) / kSlices;
     parts = (a.rows + per - 1) / per;
     // (before dx, which may stand in dy's place)
-    if (a.part)
+    if (sum)
       hipLaunchKernelGGL((norm_bwd_slices<XD, GD>), dim3((unsigned)((a.cols + kBlock - 1) / kBlock), (unsigned)parts), dim3(kBlock), 0,
                          s, a, per);
     dmt_launches(a.rows, 1024,
                  [&](unsigned first, dim3 grid) { hipLaunchKernelGGL((norm_bwd_long<XD, GD>), grid, dim3(1024), 0, s, a, first); });
   }
-  if (a.part)
+  if (sum)
     hipLaunchKernelGGL(norm_bwd_sum, dim3((unsigned)((a.cols + 63) / 64), 2), dim3(1024), 0, s, a.part, parts, a.cols, a.dgamma, a.dbeta);
 }
 
@@ -604,8 +605,9 @@ extern "C" dmt_status dmt_layer_norm_bwd(const void* x, int64_t rows, int64_t co
   if (dx == dy && dx_stride != dy_stride && rows > 1) return DMT_EINVAL;
   if (!fits(rows, cols)) return DMT_ENOTSUP;
   if (dgamma || dbeta) {
-    if (!dmt_is_at(workspace, 256)) return DMT_EINVAL;
-    if (workspace_bytes < dmt_layer_norm_bwd_workspace_bytes(rows, cols)) return DMT_ENOMEM;
+    const size_t need = dmt_layer_norm_bwd_workspace_bytes(rows, cols);      // (0: none, of no rows)
+    if (need > 0 && !dmt_is_at(workspace, 256)) return DMT_EINVAL;
+    if (workspace_bytes < need) return DMT_ENOMEM;
   }
   hipStream_t s = (hipStream_t)stream;
   Bwd a = {};
