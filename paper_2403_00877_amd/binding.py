@@ -505,6 +505,12 @@ def _vec(t: Optional[torch.Tensor], n: int, dtype) -> Optional[int]:
     return t.data_ptr()
 
 
+def _scratch(t: Optional[torch.Tensor]):
+    """Address and size of a workspace: memory of the GPU in one piece."""
+    assert t is None or (t.is_cuda and t.is_contiguous()), (t.device, tuple(t.shape), t.stride())
+    return (None, 0) if t is None else (t.data_ptr(), t.nbytes)
+
+
 def dmt_embed_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
                   first_bad: Optional[torch.Tensor] = None, stream=None) -> None:
     """out[i] = scale * table[ids[i]]; ids int32, any shape; out [ids.numel()][table's columns]."""
@@ -529,7 +535,7 @@ def dmt_embed_bwd(ids: torch.Tensor, grad: torch.Tensor, grad_table: torch.Tenso
     _check("dmt_embed_bwd", _lib.dmt_embed_bwd(
         _vec(ids, n, torch.int32), n, grad.data_ptr(), _rows(grad, n, cols), DTYPE_CODE[grad.dtype], scale,
         grad_table.data_ptr(), rows, cols, _rows(grad_table, rows, cols, torch.float32), accumulate,
-        _vec(first_bad, 1, torch.int64), workspace.data_ptr(), workspace.nbytes, _stream(stream)))
+        _vec(first_bad, 1, torch.int64), *_scratch(workspace), _stream(stream)))
 
 
 def _weights(x: torch.Tensor, *weights: Optional[torch.Tensor]):
@@ -566,7 +572,7 @@ def dmt_layer_norm_bwd(x: torch.Tensor, gamma: Optional[torch.Tensor], mean: tor
         x.data_ptr(), rows, cols, _rows(x, rows, cols), DTYPE_CODE[x.dtype], g, weight_code,
         _vec(mean, rows, torch.float32), _vec(rstd, rows, torch.float32), dy.data_ptr(), _rows(dy, rows, cols),
         DTYPE_CODE[dy.dtype], dx.data_ptr(), _rows(dx, rows, cols, dy.dtype), _vec(dgamma, cols, torch.float32),
-        _vec(dbeta, cols, torch.float32), None if workspace is None else workspace.data_ptr(), _nbytes(workspace),
+        _vec(dbeta, cols, torch.float32), *_scratch(workspace),
         _stream(stream)))
 
 
@@ -587,7 +593,7 @@ def dmt_token_logprob_fwd(x: torch.Tensor, targets: Optional[torch.Tensor] = Non
         x.data_ptr(), rows, vocab, _rows(x, rows, vocab), DTYPE_CODE[x.dtype], _vec(targets, rows, i32),
         _vec(logprob, rows, f32), _vec(entropy, rows, f32), _vec(stats, 2 * rows, f32), k, _vec(top_ids, rows * k, i32),
         _vec(top_logprobs, rows * k, f32), _vec(first_bad, 1, torch.int64),
-        None if workspace is None else workspace.data_ptr(), _nbytes(workspace), _stream(stream)))
+        *_scratch(workspace), _stream(stream)))
 
 
 def dmt_token_logprob_bwd(x: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor,
@@ -620,10 +626,10 @@ def dmt_grad_norm_workspace_bytes(grad_list) -> int:
 
 def dmt_grad_norm(grad_list, norm: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     _check("dmt_grad_norm", _lib.dmt_grad_norm(grad_list, len(grad_list), _vec(norm, 1, torch.float32),
-                                               workspace.data_ptr(), workspace.nbytes, _stream(stream)))
+                                               *_scratch(workspace), _stream(stream)))
 
 
 def dmt_grad_clip(grad_list, max_norm: float, norm: Optional[torch.Tensor], workspace: torch.Tensor,
                   stream=None) -> None:
     _check("dmt_grad_clip", _lib.dmt_grad_clip(grad_list, len(grad_list), max_norm, _vec(norm, 1, torch.float32),
-                                               workspace.data_ptr(), workspace.nbytes, _stream(stream)))
+                                               *_scratch(workspace), _stream(stream)))
