@@ -43,13 +43,6 @@ template <int DT> __device__ __forceinline__ void store1(char* p, float v) {
   else *(DMT_GLOBAL uint16_t*)p = (uint16_t)round2<DT>(v, 0.f);
 }
 
-// Loads of weights whose type only the call knows.
-__device__ __forceinline__ float load1_dyn(const void* p, int64_t at, int dt) {
-  if (dt == DMT_F32) return load1<DMT_F32>((const char*)p + at * 4);
-  if (dt == DMT_F16) return load1<DMT_F16>((const char*)p + at * 2);
-  return load1<DMT_BF16>((const char*)p + at * 2);
-}
-
 // A lane's E consecutive elements as they lie in memory.
 template <int DT, int E> struct Raw {
   static constexpr int kWords = E * EltBytes<DT>::value / 4;
@@ -183,19 +176,6 @@ template <int G> __device__ __forceinline__ float group_max(float v) {
     v = fmaxf(v, lane_xor<G / 2>(v));
   }
   return v;
-}
-
-// Sum over a block of NW waves, the same in every thread.  `smem` holds NW floats; ends with a barrier.
-template <int NW> __device__ __forceinline__ float block_sum(float v, float* smem) {
-  v = group_sum<64>(v);
-  if constexpr (NW == 1) return v;
-  if ((threadIdx.x & 63) == 0) smem[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float s = 0.f;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) s += smem[w];
-  __syncthreads();
-  return s;
 }
 
 }  // namespace dmt
