@@ -175,3 +175,24 @@ def test_gradients_far_from_zero_are_differences(dmt, power):
         close(o["logprob"][i], f64(o["logprob"][0]), 2 * (SUM + 8 * U32 * 14), "logprob")
         close(o["entropy"][i], f64(o["entropy"][0]), 2 * (2 * SUM * 9 + 8 * U32 * 64), "entropy")
         close(dx[i], f64(dx[0]), 4 * SUM * (size[0] + p) + 1e-36, "dx")
+
+
+@pytest.mark.parametrize("vocab", [1, 7, 300, 5003, 70_001])
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+def test_scores_at_the_ends_of_the_type(dmt, dt, vocab):
+    """Masks of the lowest value, each answer to the tolerance of its own score's distance."""
+    rng = np.random.default_rng(vocab + 2)
+    low, high, half = torch.finfo(DT[dt]).min, torch.finfo(DT[dt]).max, vocab // 2
+    x = [torch.from_numpy(rng.normal(size=vocab) * 2.5) for _ in range(10)]
+    x[0][:half], x[1][half:] = low, low
+    x[2][torch.from_numpy(rng.random(vocab) < 0.5)] = low
+    x[3][:] = low
+    x[4][:], x[4][vocab - 1] = low, 2.0                               # one score left: its log probability is 0
+    x[5][:], x[5][0] = low, -3.0
+    x[6][:], x[6][half] = -math.inf, low                              # beside masks of -inf, the lowest is a score
+    x[7][:] = high
+    x[8][:half], x[8][half::2] = low, high
+    x[9][half] = high
+    x = torch.stack(x).to(DT[dt]).cuda()
+    check(dmt, x, f64(x).argmax(1), (10, 0))
+    check(dmt, x, rng.integers(0, vocab, len(x)), (3,), copies=1 if vocab > 6000 else 420)
