@@ -565,7 +565,7 @@ dmt_status dmt_layer_norm_bwd(const void* x, int64_t rows, int64_t cols, int64_t
  * A score of -inf is masked: it takes no part in anything (a masked target has logprob -inf).  A row
  * whose mask leaves nothing has logprob -inf (0 without a target), entropy 0, no top items, stats {-inf, 0} and no gradient.
  * A row that holds a NaN or +inf has NaN for logprob (0 without a target) and entropy; its top items
- * are some items of the row, or -1.  Scores at the type's lowest finite value are ordinary scores.
+ * are some items of the row, or -1.  Finite scores of any size, the type's lowest value among them, are ordinary scores.
  *   x        [rows][vocab] of dtype;  targets dev int32 [rows], NULL when logprob is
  *   logprob, entropy  float32 [rows];  stats float32 [rows][2];  top_ids int32 [rows][k],
  *            top_logprobs float32 [rows][k];  any of them may be NULL (top_logprobs needs top_ids)
@@ -585,7 +585,8 @@ dmt_status dmt_token_logprob_fwd(const void* x, int64_t rows, int64_t vocab, int
 /*
  * The scores' gradient from the gradients of logprob and entropy (H), either of which may be NULL:
  *   dx_j = grad_logprob * ([j = target] - p_j) - grad_entropy * p_j * (log p_j + H)
- * Where there is no target the first term is 0.  Masked scores have gradient 0.
+ * Where there is no target the first term is 0.  Masked scores have gradient 0, whatever the rest of the row and the
+ * incoming gradients are.
  *   dx   [rows][vocab] of dtype; may be x itself (same stride)
  *   stats as dmt_token_logprob_fwd wrote it; entropy likewise, needed with grad_entropy
  */

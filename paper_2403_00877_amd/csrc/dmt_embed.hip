@@ -28,7 +28,7 @@ template <int E> __device__ __forceinline__ int piece_at(int c, int cols) { retu
 // ------------------------------------------------------------------ forward
 
 // A group of 2^log2_lpr lanes per id; a lane takes 16 bytes of the table's row at a time.  Bound by the rows' bytes out and what of the
-// table is not in a cache: 262144 ids, rows of 256 bytes, Zipf: 16.9 us, 67 MB written at 4 TB/s beside the reads; one id 1.6 us.
+// table is not in a cache: 262144 ids, rows of 256 bytes, Zipf: 18 us (17 at the least), 67 MB written at 4 TB/s beside the reads; one id 1.6 us.
 template <int TD, int OD>
 __global__ __launch_bounds__(kBlock) void embed_fwd_kernel(
     unsigned first_block, const char* __restrict__ table, int64_t rows, int cols, int64_t table_stride,

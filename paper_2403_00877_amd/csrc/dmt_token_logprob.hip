@@ -404,8 +404,8 @@ __global__ __launch_bounds__(kBlock) void logprob_join(const Fwd a) {
 // ------------------------------------------------------------------ backward
 
 // dx = p (A + B z) with p = exp2(z) / S, z to the base 2:  A = -g_lp - g_H (H - log S),  B = -g_H ln 2, S with the residue that
-// the terms here have and the kept sum has not.  A block takes a piece of a row; bound by memory: 8192 x 65536 bfloat16 363 us,
-// 5.9 TB/s, behind a forward of 210 (5.1, from past the caches).
+// the terms here have and the kept sum has not.  A block takes a piece of a row; bound by memory: 8192 x 65536 bfloat16 355 us,
+// 6.0 TB/s, behind a forward of 176 (6.1, from past the caches); in a train of twenty passes 363 and 190 to 225.
 template <int DT>
 __global__ __launch_bounds__(kBlock) void logprob_bwd(unsigned first_block, const char* x, int vocab, int64_t stride, int pieces,
                                                       const int32_t* __restrict__ targets,
