@@ -37,6 +37,11 @@
  *   dmt_token_logprob_fwd, dmt_token_logprob_bwd   log probabilities of given
  *                                items, entropy, the top k; the scores' gradient
  *   dmt_grad_norm, dmt_grad_clip   2-norm over many gradients, clipping to it
+ * For the layers of such a branch:
+ *   dmt_gated_scan_fwd, _bwd, _step, dmt_sequence_rows   gated linear recurrence over histories of any
+ *                                lengths, its gradients, one more row for states that a server holds
+ *   dmt_dropout_fwd, dmt_dropout_bwd   dropout whose mask is never stored, the residual added
+ *   dmt_expert_sort, _gather, _combine, _combine_bwd   rows sent to some of many towers and back
  *
  * Conventions
  *  - C linkage, no exceptions cross the boundary; every call returns dmt_status.
@@ -622,6 +627,157 @@ dmt_status dmt_grad_norm(const dmt_grad_tensor* tensors, int64_t count, float* n
                          void* workspace, size_t workspace_bytes, void* stream);
 dmt_status dmt_grad_clip(const dmt_grad_tensor* tensors, int64_t count, float max_norm, float* norm,
                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ------------------------------------------------------------------ the history block
+ *
+ * What mixes a user's history over time (a gated recurrence), by experts (rows sent to a few of many towers and
+ * back), and what trains such a layer (dropout).  Matrices, workspaces and first_bad are as above; outputs overlap no
+ * input unless a call says so.
+ *
+ * sequence_of: which sequence each row belongs to, dev int32 [rows], ids in [0, sequences), the rows of a sequence
+ * one after another (a sequence may have none).  A row with a negative id belongs to none: it takes no part, its outputs are
+ * zeros, and its inputs may hold anything.  So may one with an id >= sequences, which first_bad reports.  NULL: `sequences` sequences of
+ * rows / sequences rows each.  Rows of one id with others between them are that many pieces, each a sequence
+ * from the id's initial state on; which of them the id's row of a per-sequence output holds is not said.
+ */
+
+/*
+ * sequence_of from a jagged batch's offsets: sequence_of[r] = b where offsets[b] <= r < offsets[b + 1], -1 for rows outside
+ * [offsets[0], offsets[sequences]).
+ *   offsets  dev int64 [sequences + 1], ascending; where they do not ascend, the rows' ids are some ids, and
+ *            first_bad is lowered to the smallest b with offsets[b + 1] < offsets[b]
+ * DMT_ENOTSUP for rows or sequences beyond 2^30.
+ */
+dmt_status dmt_sequence_rows(const int64_t* offsets, int64_t sequences, int64_t rows, int32_t* sequence_of,
+                             int64_t* first_bad, void* stream);
+
+typedef enum {
+  DMT_SCAN_COUPLED = 0, /* h_t = f_t h_{t-1} + (1 - f_t) value_t */
+  DMT_SCAN_FREE = 1     /* h_t = f_t h_{t-1} + value_t           */
+} dmt_scan_form;
+
+/*
+ * Gated linear recurrence along the rows of each sequence, channel by channel, with f = 1 / (1 + exp(-gate)):
+ *   h_t = f_t h_{t-1} + u_t,   u as `form` says,   h before the first row = initial[sequence] (NULL: 0)
+ *   gate, value, h   [rows][cols] of dtype
+ *   initial, final   float32 [sequences][cols]; final: the state after the last row; rows of sequences without rows are
+ *                    not written; either may be NULL; they must not overlap
+ *   kept             what dmt_gated_scan_bwd reads, of dmt_gated_scan_kept_bytes(rows, cols) bytes, 256-byte aligned; NULL: nothing is kept
+ *   workspace        of dmt_gated_scan_workspace_bytes(rows, cols), for the forward as for the backward
+ * States are float32 whatever dtype is; only h is rounded.  A NaN or an infinity stays in its sequence and channel.
+ * cols >= 1, rows >= 0, sequences >= 0; without sequence_of DMT_EINVAL unless sequences divides rows.  DMT_ENOTSUP for
+ * rows or sequences beyond 2^30, cols beyond 2^24.
+ */
+size_t dmt_gated_scan_workspace_bytes(int64_t rows, int64_t cols);
+size_t dmt_gated_scan_kept_bytes(int64_t rows, int64_t cols);
+dmt_status dmt_gated_scan_fwd(const void* gate, int64_t gate_stride, const void* value, int64_t value_stride,
+                              int64_t rows, int64_t cols, int32_t dtype, int32_t form,
+                              const int32_t* sequence_of, int64_t sequences, const float* initial, void* h,
+                              int64_t h_stride, float* final, void* kept, size_t kept_bytes,
+                              int64_t* first_bad, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients.  With l_t = dh_t + f_{t+1} l_{t+1} (at a last row: dh_t + dfinal):
+ *   dvalue_t = (1 - f_t) l_t (free: l_t),   dgate_t = l_t (h_{t-1} - value_t) f_t (1 - f_t) (free: l_t h_{t-1} f_t (1 - f_t)),
+ *   dinitial = f_1 l_1
+ *   gate, value, form, sequence_of, sequences, initial   as the forward had them;  kept as it left it
+ *   dh, dgate, dvalue   [rows][cols] of grad_dtype (dtype or DMT_F32)
+ *   dfinal, dinitial    float32 [sequences][cols], either may be NULL (dfinal: 0); rows of dinitial of sequences
+ *                       without rows are not written
+ */
+dmt_status dmt_gated_scan_bwd(const void* gate, int64_t gate_stride, const void* value, int64_t value_stride,
+                              int64_t rows, int64_t cols, int32_t dtype, int32_t form,
+                              const int32_t* sequence_of, int64_t sequences, const float* initial,
+                              const void* kept, size_t kept_bytes, const void* dh, int64_t dh_stride,
+                              int32_t grad_dtype, const float* dfinal, void* dgate, int64_t dgate_stride,
+                              void* dvalue, int64_t dvalue_stride, float* dinitial, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
+ * One row more for some of the sequences whose states a server holds:
+ *   h[i] = f_i * state[slots[i]] + u_i,   new_state[slots[i]] = h[i] before its rounding
+ *   gate, value, h     [rows][cols] of dtype
+ *   slots              dev int32 [rows]; NULL: row i's is i (then states >= rows).  A negative slot: no sequence, h is zeros.
+ *                      One >= states, or that an earlier row of the call names too, is treated the same and
+ *                      reported in first_bad (the row)
+ *   state, new_state   float32 [states][cols]; new_state may be state itself; rows that no slot names are not written
+ * rows >= 0, cols >= 1, states >= 0; DMT_ENOTSUP for rows beyond 65536 with slots (2^30 without), states beyond 2^30, cols beyond 2^24.
+ */
+dmt_status dmt_gated_scan_step(const void* gate, int64_t gate_stride, const void* value, int64_t value_stride,
+                               int64_t rows, int64_t cols, int32_t dtype, int32_t form, const int32_t* slots,
+                               const float* state, float* new_state, int64_t states, void* h,
+                               int64_t h_stride, int64_t* first_bad, void* stream);
+
+/*
+ * Dropout: y = residual + (x where an element stays, else 0) / (1 - q), and the same for gradients:
+ * dx = (dy where the element stayed, else 0) / (1 - q).  No mask is stored: whether element (row, col) stays is a function of
+ * rng, site, row and col alone, not of type, stride or launch.  An element is left out where its 16 bits are below
+ * m = floor(65536 p + 1/2), so that q = m / 65536; p = 1 leaves out all.  The bits are half-word col % 8 (low halves
+ * first) of the four words of Philox4x32-10 (Salmon et al. 2011) under key (seed's low word, high word) at counter
+ * (site * 2^21 + col / 8, row, step's low word, high word).
+ *   x, residual, y   [rows][cols] of dtype; residual may be NULL; y may be x or residual itself (same stride)
+ *   dy, dx           [rows][cols] of dtype (any); dx may be dy itself (same stride)
+ *   rng              dev int64 [2]: seed and step, read by the kernel (a captured graph draws anew when it is changed)
+ *   site             0 ... 2047: which of a model's dropouts
+ * An element that is left out is 0 whatever it holds.  p in [0, 1]; DMT_ENOTSUP for rows beyond 2^31 - 1, cols beyond 2^24.
+ */
+dmt_status dmt_dropout_fwd(const void* x, int64_t rows, int64_t cols, int64_t x_stride, int32_t dtype,
+                           const void* residual, int64_t residual_stride, float p, const int64_t* rng,
+                           int32_t site, void* y, int64_t y_stride, void* stream);
+dmt_status dmt_dropout_bwd(const void* dy, int64_t rows, int64_t cols, int64_t dy_stride, int32_t dtype, float p,
+                           const int64_t* rng, int32_t site, void* dx, int64_t dx_stride, void* stream);
+
+/*
+ * Rows sent to experts and back.  Each of n tokens names k experts; assignment a = i * k + j is token i's j-th.
+ * dmt_expert_sort orders the assignments by expert, those of one expert as they come, and gives each a row:
+ *   counts[e]   assignments that name e
+ *   offsets[e]  e's first row: capacity = 0: the sum of the counts before e (rows = n * k); else e * capacity (rows =
+ *               num_experts * capacity), and e takes its first `capacity` assignments, the others are dropped
+ *   slot[a]     assignment a's row; -1 where it names no expert (negative; >= num_experts: reported in first_bad) or is dropped
+ *   source[r]   row r's assignment; -1 where there is none
+ * With a capacity the rows are the tower-major tensor of a plan with num_experts towers and B = capacity, so
+ * dmt_tower_module_fwd and dmt_tower_module_bwd are the experts' products.
+ *   experts dev int32 [n][k]; slot int32 [n][k]; source int32 [rows]; offsets int32 [num_experts + 1]; counts int32
+ *   [num_experts]; offsets and counts may be NULL
+ *   workspace of dmt_expert_sort_workspace_bytes(n, k, num_experts)
+ * n >= 0, k >= 1, 1 <= num_experts <= DMT_EXPERT_MAX, capacity >= 0; DMT_ENOTSUP for more experts, and for n * k or rows beyond 2^31 - 1.
+ */
+#define DMT_EXPERT_MAX 1024
+size_t dmt_expert_sort_workspace_bytes(int64_t n, int64_t k, int64_t num_experts);
+dmt_status dmt_expert_sort(const int32_t* experts, int64_t n, int64_t k, int64_t num_experts,
+                           int64_t capacity, int32_t* slot, int32_t* source, int32_t* offsets,
+                           int32_t* counts, int64_t* first_bad, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/*
+ * out[slot[i][j]] = x[i];  rows without an assignment get zeros.  (Its gradient: dmt_expert_combine without weights.)
+ *   x [n][cols], out [rows][cols] of dtype; slot [n][k] and source [rows] as dmt_expert_sort wrote them
+ * DMT_ENOTSUP for n * k or rows beyond 2^31 - 1, cols beyond 2^24.
+ */
+dmt_status dmt_expert_gather(const void* x, int64_t n, int64_t cols, int64_t x_stride, int32_t dtype,
+                             const int32_t* slot, int64_t k, const int32_t* source, int64_t rows, void* out,
+                             int64_t out_stride, void* stream);
+
+/*
+ * y[i] = sum over j, ascending, of weights[i][j] * z[slot[i][j]]  (weights NULL: 1); assignments without a row count nothing.
+ *   z [rows][cols] of dtype; y [n][cols] of y_dtype; weights dev float32 [n][k]; slot as above (an entry >= rows: none)
+ */
+dmt_status dmt_expert_combine(const void* z, int64_t rows, int64_t cols, int64_t z_stride, int32_t dtype,
+                              const int32_t* slot, int64_t n, int64_t k, const float* weights, void* y,
+                              int64_t y_stride, int32_t y_dtype, void* stream);
+
+/*
+ * Its gradients:  dz[slot[i][j]] = weights[i][j] * dy[i], zeros for rows without an assignment;
+ *                 dweights[i][j] = sum over columns of dy[i] * z[slot[i][j]], 0 where there is no row
+ *   dy [n][cols], dz [rows][cols] of grad_dtype (dtype or DMT_F32); z as the forward had it
+ *   dweights float32 [n][k]; either output may be NULL (without dweights z is not read and may be NULL, without dz source may be)
+ */
+dmt_status dmt_expert_combine_bwd(const void* dy, int64_t n, int64_t cols, int64_t dy_stride,
+                                  int32_t grad_dtype, const void* z, int64_t rows, int64_t z_stride,
+                                  int32_t dtype, const int32_t* slot, int64_t k, const int32_t* source,
+                                  const float* weights, void* dz, int64_t dz_stride, float* dweights,
+                                  void* stream);
 
 /*
  * Synchronise `stream` and report what the kernels since the last call found wrong with

@@ -16,4 +16,7 @@ from .binding import (  # noqa: F401
     dmt_embed_fwd, dmt_embed_bwd_workspace_bytes, dmt_embed_bwd, dmt_layer_norm_fwd,
     dmt_layer_norm_bwd_workspace_bytes, dmt_layer_norm_bwd, dmt_token_logprob_workspace_bytes,
     dmt_token_logprob_fwd, dmt_token_logprob_bwd, make_grad_list, dmt_grad_norm_workspace_bytes,
-    dmt_grad_norm, dmt_grad_clip)
+    dmt_grad_norm, dmt_grad_clip, dmt_sequence_rows, dmt_gated_scan_workspace_bytes, dmt_gated_scan_kept_bytes,
+    dmt_gated_scan_fwd, dmt_gated_scan_bwd, dmt_gated_scan_step, dmt_dropout_fwd, dmt_dropout_bwd,
+    dmt_expert_sort_workspace_bytes, dmt_expert_sort, dmt_expert_gather, dmt_expert_combine, dmt_expert_combine_bwd,
+    DMT_EXPERT_MAX)

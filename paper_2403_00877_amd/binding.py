@@ -128,6 +128,21 @@ def _load() -> ctypes.CDLL:
     lib.dmt_grad_norm_workspace_bytes.restype = sz
     lib.dmt_grad_norm.argtypes = [vp, i64, vp, vp, sz, vp]
     lib.dmt_grad_clip.argtypes = [vp, i64, f32, vp, vp, sz, vp]
+    lib.dmt_sequence_rows.argtypes = [vp, i64, i64, vp, vp, vp]
+    for f in (lib.dmt_gated_scan_workspace_bytes, lib.dmt_gated_scan_kept_bytes):
+        f.argtypes, f.restype = [i64, i64], sz
+    lib.dmt_gated_scan_fwd.argtypes = [vp, i64, vp, i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp, sz, vp, vp, sz, vp]
+    lib.dmt_gated_scan_bwd.argtypes = [vp, i64, vp, i64, i64, i64, i32, i32, vp, i64, vp, vp, sz, vp, i64, i32, vp, vp, i64,
+                                       vp, i64, vp, vp, sz, vp]
+    lib.dmt_gated_scan_step.argtypes = [vp, i64, vp, i64, i64, i64, i32, i32, vp, vp, vp, i64, vp, i64, vp, vp]
+    lib.dmt_dropout_fwd.argtypes = [vp, i64, i64, i64, i32, vp, i64, f32, vp, i32, vp, i64, vp]
+    lib.dmt_dropout_bwd.argtypes = [vp, i64, i64, i64, i32, f32, vp, i32, vp, i64, vp]
+    lib.dmt_expert_sort_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.dmt_expert_sort_workspace_bytes.restype = sz
+    lib.dmt_expert_sort.argtypes = [vp, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.dmt_expert_gather.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp]
+    lib.dmt_expert_combine.argtypes = [vp, i64, i64, i64, i32, vp, i64, i64, vp, vp, i64, i32, vp]
+    lib.dmt_expert_combine_bwd.argtypes = [vp, i64, i64, i64, i32, vp, i64, i64, i32, vp, i64, vp, vp, vp, i64, vp, vp]
     return lib
 
 
@@ -146,9 +161,15 @@ EXPORTS = ["dmt_status_str", "dmt_plan_create", "dmt_plan_destroy", "dmt_plan_la
            "dmt_embed_fwd", "dmt_embed_bwd_workspace_bytes", "dmt_embed_bwd", "dmt_layer_norm_fwd",
            "dmt_layer_norm_bwd_workspace_bytes", "dmt_layer_norm_bwd", "dmt_token_logprob_workspace_bytes",
            "dmt_token_logprob_fwd", "dmt_token_logprob_bwd", "dmt_grad_norm_workspace_bytes", "dmt_grad_norm",
-           "dmt_grad_clip"]
+           "dmt_grad_clip", "dmt_sequence_rows", "dmt_gated_scan_workspace_bytes", "dmt_gated_scan_kept_bytes",
+           "dmt_gated_scan_fwd", "dmt_gated_scan_bwd", "dmt_gated_scan_step", "dmt_dropout_fwd", "dmt_dropout_bwd",
+           "dmt_expert_sort_workspace_bytes", "dmt_expert_sort", "dmt_expert_gather", "dmt_expert_combine",
+           "dmt_expert_combine_bwd"]
 
 DMT_K_COUNT = 15
+DMT_SCAN_COUPLED, DMT_SCAN_FREE = 0, 1
+SCAN_FORM_CODE = {"coupled": DMT_SCAN_COUPLED, "free": DMT_SCAN_FREE}
+DMT_EXPERT_MAX = 1024
 TP_STRATEGY_CODE = {"diverse": 0, "coherent": 1}
 
 
@@ -633,3 +654,157 @@ def dmt_grad_clip(grad_list, max_norm: float, norm: Optional[torch.Tensor], work
                   stream=None) -> None:
     _check("dmt_grad_clip", _lib.dmt_grad_clip(grad_list, len(grad_list), max_norm, _vec(norm, 1, torch.float32),
                                                *_scratch(workspace), _stream(stream)))
+
+
+# ---------------------------------------------------------------- the history block
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """The call's stream is the current device's: so are its tensors."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or (t.is_cuda and t.get_device() == device), (t.device, device)
+
+
+def dmt_sequence_rows(offsets: torch.Tensor, sequence_of: torch.Tensor, first_bad: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+    """sequence_of[r] = b where offsets[b] <= r < offsets[b + 1], else -1; offsets int64, one more than there are sequences."""
+    _here(offsets, sequence_of, first_bad)
+    n, rows = offsets.numel(), sequence_of.numel()
+    _check("dmt_sequence_rows", _lib.dmt_sequence_rows(
+        _vec(offsets, n, torch.int64), n - 1, rows, _vec(sequence_of, rows, torch.int32), _vec(first_bad, 1, torch.int64),
+        _stream(stream)))
+
+
+def dmt_gated_scan_workspace_bytes(rows: int, cols: int) -> int:
+    return int(_lib.dmt_gated_scan_workspace_bytes(rows, cols))
+
+
+def dmt_gated_scan_kept_bytes(rows: int, cols: int) -> int:
+    return int(_lib.dmt_gated_scan_kept_bytes(rows, cols))
+
+
+def dmt_gated_scan_fwd(gate: torch.Tensor, value: torch.Tensor, h: torch.Tensor, workspace: Optional[torch.Tensor],
+                       form: str = "coupled", sequence_of: Optional[torch.Tensor] = None, sequences: int = 1,
+                       initial: Optional[torch.Tensor] = None, final: Optional[torch.Tensor] = None,
+                       kept: Optional[torch.Tensor] = None, first_bad: Optional[torch.Tensor] = None, stream=None) -> None:
+    """h_t = f h_{t-1} + (1 - f) value_t (form "free": + value_t), f = sigmoid(gate_t), along the rows of each sequence."""
+    rows, cols = gate.shape
+    _here(gate, value, h, workspace, sequence_of, initial, final, kept, first_bad)
+    f32, states = torch.float32, sequences * cols
+    _check("dmt_gated_scan_fwd", _lib.dmt_gated_scan_fwd(
+        gate.data_ptr(), _rows(gate, rows, cols), value.data_ptr(), _rows(value, rows, cols, gate.dtype), rows, cols,
+        DTYPE_CODE[gate.dtype], SCAN_FORM_CODE[form], _vec(sequence_of, rows, torch.int32), sequences,
+        _vec(initial, states, f32), h.data_ptr(), _rows(h, rows, cols, gate.dtype), _vec(final, states, f32),
+        *_scratch(kept), _vec(first_bad, 1, torch.int64), *_scratch(workspace), _stream(stream)))
+
+
+def dmt_gated_scan_bwd(gate: torch.Tensor, value: torch.Tensor, dh: torch.Tensor, dgate: torch.Tensor,
+                       dvalue: torch.Tensor, kept: torch.Tensor, workspace: Optional[torch.Tensor], form: str = "coupled",
+                       sequence_of: Optional[torch.Tensor] = None, sequences: int = 1,
+                       initial: Optional[torch.Tensor] = None, dfinal: Optional[torch.Tensor] = None,
+                       dinitial: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of gate, value and initial from those of h and final; kept as the forward left it."""
+    rows, cols = gate.shape
+    _here(gate, value, dh, dgate, dvalue, kept, workspace, sequence_of, initial, dfinal, dinitial)
+    f32, states = torch.float32, sequences * cols
+    _check("dmt_gated_scan_bwd", _lib.dmt_gated_scan_bwd(
+        gate.data_ptr(), _rows(gate, rows, cols), value.data_ptr(), _rows(value, rows, cols, gate.dtype), rows, cols,
+        DTYPE_CODE[gate.dtype], SCAN_FORM_CODE[form], _vec(sequence_of, rows, torch.int32), sequences,
+        _vec(initial, states, f32), *_scratch(kept), dh.data_ptr(), _rows(dh, rows, cols), DTYPE_CODE[dh.dtype],
+        _vec(dfinal, states, f32), dgate.data_ptr(), _rows(dgate, rows, cols, dh.dtype), dvalue.data_ptr(),
+        _rows(dvalue, rows, cols, dh.dtype), _vec(dinitial, states, f32), *_scratch(workspace), _stream(stream)))
+
+
+def dmt_gated_scan_step(gate: torch.Tensor, value: torch.Tensor, state: torch.Tensor, new_state: torch.Tensor,
+                        h: torch.Tensor, slots: Optional[torch.Tensor] = None, form: str = "coupled",
+                        first_bad: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One row more for the sequences whose states (float32 [states][cols]) slots names; new_state may be state itself."""
+    rows, cols = gate.shape
+    states = state.shape[0]
+    _here(gate, value, state, new_state, h, slots, first_bad)
+    _check("dmt_gated_scan_step", _lib.dmt_gated_scan_step(
+        gate.data_ptr(), _rows(gate, rows, cols), value.data_ptr(), _rows(value, rows, cols, gate.dtype), rows, cols,
+        DTYPE_CODE[gate.dtype], SCAN_FORM_CODE[form], _vec(slots, rows, torch.int32),
+        _vec(state, states * cols, torch.float32), _vec(new_state, states * cols, torch.float32), states, h.data_ptr(),
+        _rows(h, rows, cols, gate.dtype), _vec(first_bad, 1, torch.int64), _stream(stream)))
+
+
+def dmt_dropout_fwd(x: torch.Tensor, p: float, rng: torch.Tensor, y: torch.Tensor,
+                    residual: Optional[torch.Tensor] = None, site: int = 0, stream=None) -> None:
+    """y = residual + (x where it stays) / (1 - p); rng int64 [2] (seed, step) on the GPU."""
+    rows, cols = x.shape
+    _here(x, rng, y, residual)
+    res, res_stride = (None, 0) if residual is None else (residual.data_ptr(), _rows(residual, rows, cols, x.dtype))
+    _check("dmt_dropout_fwd", _lib.dmt_dropout_fwd(
+        x.data_ptr(), rows, cols, _rows(x, rows, cols), DTYPE_CODE[x.dtype], res, res_stride, p, _vec(rng, 2, torch.int64),
+        site, y.data_ptr(), _rows(y, rows, cols, x.dtype), _stream(stream)))
+
+
+def dmt_dropout_bwd(dy: torch.Tensor, p: float, rng: torch.Tensor, dx: torch.Tensor, site: int = 0, stream=None) -> None:
+    """dx = (dy where the element stayed) / (1 - p), for the same rng and site as the forward."""
+    rows, cols = dy.shape
+    _here(dy, rng, dx)
+    _check("dmt_dropout_bwd", _lib.dmt_dropout_bwd(
+        dy.data_ptr(), rows, cols, _rows(dy, rows, cols), DTYPE_CODE[dy.dtype], p, _vec(rng, 2, torch.int64), site,
+        dx.data_ptr(), _rows(dx, rows, cols, dy.dtype), _stream(stream)))
+
+
+def dmt_expert_sort_workspace_bytes(n: int, k: int, num_experts: int) -> int:
+    return int(_lib.dmt_expert_sort_workspace_bytes(n, k, num_experts))
+
+
+def dmt_expert_sort(experts: torch.Tensor, num_experts: int, slot: torch.Tensor, source: torch.Tensor,
+                    offsets: Optional[torch.Tensor], counts: Optional[torch.Tensor], workspace: Optional[torch.Tensor],
+                    capacity: int = 0, first_bad: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Assignments [n][k] ordered by expert: slot [n][k], source [n * k, or num_experts * capacity], all int32."""
+    n, k = experts.shape
+    _here(experts, slot, source, offsets, counts, workspace, first_bad)
+    i32 = torch.int32
+    _check("dmt_expert_sort", _lib.dmt_expert_sort(
+        _vec(experts, n * k, i32), n, k, num_experts, capacity, _vec(slot, n * k, i32),
+        _vec(source, num_experts * capacity if capacity else n * k, i32), _vec(offsets, num_experts + 1, i32),
+        _vec(counts, num_experts, i32), _vec(first_bad, 1, torch.int64), *_scratch(workspace), _stream(stream)))
+
+
+def _slots(slot: torch.Tensor):
+    """Address of [n][k] slots, n, k."""
+    n, k = slot.shape
+    return _vec(slot, n * k, torch.int32), n, k
+
+
+def dmt_expert_gather(x: torch.Tensor, slot: torch.Tensor, source: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """out[slot[i][j]] = x[i], zeros in rows without an assignment."""
+    at, n, k = _slots(slot)
+    rows, cols = out.shape
+    _here(x, slot, source, out)
+    _check("dmt_expert_gather", _lib.dmt_expert_gather(
+        x.data_ptr(), n, cols, _rows(x, n, cols, out.dtype), DTYPE_CODE[x.dtype], at, k, _vec(source, rows, torch.int32),
+        rows, out.data_ptr(), _rows(out, rows, cols), _stream(stream)))
+
+
+def dmt_expert_combine(z: torch.Tensor, slot: torch.Tensor, weights: Optional[torch.Tensor], y: torch.Tensor,
+                       stream=None) -> None:
+    """y[i] = the sum over j of weights[i][j] * z[slot[i][j]] (weights None: 1)."""
+    at, n, k = _slots(slot)
+    rows, cols = z.shape
+    _here(z, slot, weights, y)
+    _check("dmt_expert_combine", _lib.dmt_expert_combine(
+        z.data_ptr(), rows, cols, _rows(z, rows, cols), DTYPE_CODE[z.dtype], at, n, k, _vec(weights, n * k, torch.float32),
+        y.data_ptr(), _rows(y, n, cols), DTYPE_CODE[y.dtype], _stream(stream)))
+
+
+def dmt_expert_combine_bwd(dy: torch.Tensor, z: Optional[torch.Tensor], slot: torch.Tensor,
+                           source: Optional[torch.Tensor], weights: Optional[torch.Tensor],
+                           dz: Optional[torch.Tensor] = None, dweights: Optional[torch.Tensor] = None,
+                           stream=None) -> None:
+    """dz[slot[i][j]] = weights[i][j] * dy[i], zeros elsewhere; dweights[i][j] = dy[i] . z[slot[i][j]]."""
+    at, n, k = _slots(slot)
+    cols = dy.shape[1]
+    _here(dy, z, slot, source, weights, dz, dweights)
+    rows = z.shape[0] if z is not None else dz.shape[0] if dz is not None else 0
+    z_at, z_stride, dtype = (None, cols, dy.dtype) if z is None else (z.data_ptr(), _rows(z, rows, cols), z.dtype)
+    dz_at, dz_stride = (None, cols) if dz is None else (dz.data_ptr(), _rows(dz, rows, cols, dy.dtype))
+    _check("dmt_expert_combine_bwd", _lib.dmt_expert_combine_bwd(
+        dy.data_ptr(), n, cols, _rows(dy, n, cols), DTYPE_CODE[dy.dtype], z_at, rows, z_stride, DTYPE_CODE[dtype], at, k,
+        _vec(source, rows, torch.int32), _vec(weights, n * k, torch.float32), dz_at, dz_stride,
+        _vec(dweights, n * k, torch.float32), _stream(stream)))

@@ -1,0 +1,353 @@
+// dmt_expert_sort, dmt_expert_gather, dmt_expert_combine, dmt_expert_combine_bwd: rows sent to experts and back.
+//
+// The order is a counting sort with the expert as the only digit: counts of a tile of assignments, then places.  A tile is a
+// block's; there are at most 64 tiles, so that a block finds the counts before it by adding up to 64 rows of counts itself and no
+// launch of its own scans them.  Inside a tile every wave has a stretch of its own and ranks 64 assignments at a time: the
+// lanes that name the same expert are found with one ballot a bit of the expert's number.  Places depend on the assignments'
+// order alone.  One tile needs one launch.
+#include <algorithm>
+
+#include "dmt_internal.h"
+#include "dmt_rows.h"
+
+namespace {
+
+constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / 64, kTiles = 64, kBlock = 256;
+
+struct Sort {
+  const int32_t* experts;
+  int64_t m, rows;              // assignments, rows of the order
+  int64_t stretch;              // assignments a wave has, a multiple of 64
+  int E, bits, tiles;
+  int64_t capacity;
+  int32_t *slot, *source, *offsets, *counts, *part;      // part [tiles][E]
+  unsigned long long* first_bad;
+};
+
+// The wave's stretch of the tile's assignments.
+__device__ __forceinline__ void stretch_of(const Sort& a, int64_t& from, int64_t& to) {
+  from = min(a.m, ((int64_t)blockIdx.x * kSortWaves + (threadIdx.x >> 6)) * a.stretch);
+  to = min(a.m, from + a.stretch);
+}
+
+// Counts of the wave's assignments by expert, added to count[E] (LDS, zero).
+__device__ __forceinline__ void count_stretch(const Sort& a, int* count) {
+  int64_t from, to;
+  stretch_of(a, from, to);
+  for (int64_t i = from + (threadIdx.x & 63); i < to; i += 64) {
+    const int e = a.experts[i];
+    if ((uint32_t)e < (uint32_t)a.E) atomicAdd(&count[e], 1);
+    else if (e >= 0 && a.first_bad) atomicMin(a.first_bad, (unsigned long long)i);
+  }
+}
+
+__global__ __launch_bounds__(kSortBlock) void expert_count(const Sort a) {
+  extern __shared__ int lds[];
+  for (int e = threadIdx.x; e < a.E; e += kSortBlock) lds[e] = 0;
+  __syncthreads();
+  count_stretch(a, lds);
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += kSortBlock) a.part[(int64_t)blockIdx.x * a.E + e] = lds[e];
+}
+
+// LDS: place [waves][E], total [E], begin [E], and a word a wave.
+__global__ __launch_bounds__(kSortBlock) void expert_place(const Sort a) {
+  extern __shared__ int lds[];
+  const int E = a.E, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  int *place = lds, *total = place + kSortWaves * E, *begin = total + E, *sums = begin + E;
+  for (int i = threadIdx.x; i < kSortWaves * E; i += kSortBlock) place[i] = 0;
+  __syncthreads();
+  count_stretch(a, place + wave * E);
+  __syncthreads();
+  // an expert a thread (E <= kSortBlock): its assignments in all, those of the tiles before, those of the waves before
+  const int e = threadIdx.x;
+  int all = 0, before = 0;
+  if (e < E) {
+    if (a.tiles > 1)
+      for (int t = 0; t < a.tiles; ++t) {
+        const int c = a.part[(int64_t)t * E + e];
+        all += c;
+        before += t < (int)blockIdx.x ? c : 0;
+      }
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = place[w * E + e];
+      place[w * E + e] = before;
+      before += c;
+      if (a.tiles == 1) all += c;
+    }
+  }
+  uint32_t sum;
+  const int at = (int)dmt::block_exclusive_scan<kSortWaves>((uint32_t)all, (uint32_t*)sums, sum);
+  if (e < E) {
+    total[e] = all;
+    begin[e] = a.capacity ? (int)(e * a.capacity) : at;
+    if (blockIdx.x == 0) {
+      if (a.offsets) a.offsets[e] = begin[e];
+      if (a.counts) a.counts[e] = all;
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0 && a.offsets) a.offsets[E] = a.capacity ? (int)(E * a.capacity) : (int)sum;
+  __syncthreads();
+  int64_t from, to;
+  stretch_of(a, from, to);
+  for (int64_t i0 = from; i0 < to; i0 += 64) {
+    const int64_t i = i0 + lane;
+    const int x = i < to ? a.experts[i] : -1;
+    const bool named = (uint32_t)x < (uint32_t)E;
+    uint64_t same = __ballot(named);
+    for (int b = 0; b < a.bits; ++b) {
+      const uint64_t set = __ballot((x >> b) & 1);
+      same &= (x >> b) & 1 ? set : ~set;
+    }
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    int base = 0;
+    if (named && rank == 0) base = atomicAdd(&place[wave * E + x], (int)__popcll(same));
+    base = __shfl(base, named ? __ffsll((unsigned long long)same) - 1 : lane);
+    if (i < to) {
+      int64_t row = -1;
+      if (named) {
+        const int64_t r = (int64_t)base + rank;
+        if (!a.capacity || r < a.capacity) row = begin[x] + r;
+      }
+      a.slot[i] = (int)row;
+      if (row >= 0) a.source[row] = (int)i;
+    }
+  }
+  // rows without an assignment: behind the last one (of an expert)
+  for (int64_t r = (int64_t)blockIdx.x * kSortBlock + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * kSortBlock) {
+    if (a.capacity) {
+      const int x = (int)(r / a.capacity);
+      if (r - x * a.capacity >= total[x]) a.source[r] = -1;
+    } else if (r >= (int64_t)sum) {
+      a.source[r] = -1;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ rows there and back
+
+struct Move {
+  const char *x, *z;
+  char* out;
+  int64_t x_stride, z_stride, out_stride, n, rows;
+  const int32_t *slot, *source;
+  const float* weights;
+  float* dweights;
+  int cols, k;
+};
+
+// Pieces of 16 bytes at a time; a group of 64 lanes has a row.
+template <int EB>
+__global__ __launch_bounds__(kBlock) void expert_gather(const Move a, unsigned first) {
+  constexpr int DT = EB == 4 ? DMT_F32 : DMT_F16, E = 16 / EB;
+  const int64_t r = (int64_t)(first + blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
+  if (r >= a.rows) return;
+  const int s = a.source[r];
+  const bool there = s >= 0 && s / a.k < a.n;
+  const char* from = a.x + (there ? (int64_t)(s / a.k) * a.x_stride : 0) * EB;
+  char* to = a.out + r * a.out_stride * EB;
+  for (int c = (threadIdx.x & 63) * E; c < a.cols; c += 64 * E) {
+    const int valid = min(E, a.cols - c);
+    dmt::Raw<DT, E> v = {};
+    if (there) v = dmt::load_raw<DT, E>(from + (int64_t)c * EB, valid);
+    if (valid == E) {
+      const dmt::dmt_u32x4 w = {v.w[0], v.w[1], v.w[2], v.w[3]};
+      *(DMT_GLOBAL typename dmt::Piece<EB>::v4*)(to + (int64_t)c * EB) = w;
+    } else {
+      for (int i = 0; i < valid; ++i) {
+        if constexpr (EB == 4) *(DMT_GLOBAL uint32_t*)(to + (int64_t)(c + i) * 4) = v.w[i];
+        else *(DMT_GLOBAL uint16_t*)(to + (int64_t)(c + i) * 2) = (uint16_t)(v.w[i / 2] >> i % 2 * 16);
+      }
+    }
+  }
+}
+
+template <int DT, int OD>
+__global__ __launch_bounds__(kBlock) void expert_combine(const Move a, unsigned first) {
+  constexpr int EB = dmt::EltBytes<DT>::value, OB = dmt::EltBytes<OD>::value, E = 8;
+  const int64_t i = (int64_t)(first + blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
+  if (i >= a.n) return;
+  for (int c = (threadIdx.x & 63) * E; c < a.cols; c += 64 * E) {
+    const int valid = min(E, a.cols - c);
+    float sum[E] = {};
+    for (int j = 0; j < a.k; ++j) {
+      const int64_t s = a.slot[i * a.k + j];
+      if (s < 0 || s >= a.rows) continue;
+      const float w = a.weights ? a.weights[i * a.k + j] : 1.f;
+      float v[E];
+      dmt::load_elems<DT, E>(a.z + (s * a.z_stride + c) * EB, valid, v);
+#pragma unroll
+      for (int q = 0; q < E; ++q) sum[q] = fmaf(w, v[q], sum[q]);
+    }
+    dmt::store_elems<OD, E>(a.out + (i * a.out_stride + c) * OB, valid, sum);
+  }
+}
+
+// x is dy here, out dz.
+template <int DT, int GD>
+__global__ __launch_bounds__(kBlock) void expert_combine_bwd(const Move a, unsigned first) {
+  constexpr int EB = dmt::EltBytes<DT>::value, GB = dmt::EltBytes<GD>::value, E = 8;
+  const int64_t i = (int64_t)(first + blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
+  if (i >= a.n) return;
+  const int lane = threadIdx.x & 63;
+  for (int j = 0; j < a.k; ++j) {
+    const int64_t s = a.slot[i * a.k + j];
+    const bool there = s >= 0 && s < a.rows;
+    const float w = a.weights ? a.weights[i * a.k + j] : 1.f;
+    float dot = 0.f;
+    for (int c = lane * E; there && c < a.cols; c += 64 * E) {
+      const int valid = min(E, a.cols - c);
+      float g[E], v[E];
+      dmt::load_elems<GD, E>(a.x + (i * a.x_stride + c) * GB, valid, g);
+      if (a.dweights) {
+        dmt::load_elems<DT, E>(a.z + (s * a.z_stride + c) * EB, valid, v);
+#pragma unroll
+        for (int q = 0; q < E; ++q) dot = fmaf(g[q], v[q], dot);
+      }
+      if (a.out) {
+#pragma unroll
+        for (int q = 0; q < E; ++q) g[q] *= w;
+        dmt::store_elems<GD, E>(a.out + (s * a.out_stride + c) * GB, valid, g);
+      }
+    }
+    if (a.dweights) {
+      dot = dmt::group_sum<64>(dot);
+      if (lane == 0) a.dweights[i * a.k + j] = dot;
+    }
+  }
+}
+
+// Zeros into the rows without an assignment.
+template <int EB>
+__global__ __launch_bounds__(kBlock) void expert_clear(const Move a, unsigned first) {
+  constexpr int DT = EB == 4 ? DMT_F32 : DMT_F16, E = 16 / EB;
+  const int64_t r = (int64_t)(first + blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
+  if (r >= a.rows || a.source[r] >= 0) return;
+  const float zero[E] = {};
+  for (int c = (threadIdx.x & 63) * E; c < a.cols; c += 64 * E)
+    dmt::store_elems<DT, E>(a.out + (r * a.out_stride + c) * EB, min(E, a.cols - c), zero);
+}
+
+template <int V> struct Int { static constexpr int value = V; };
+template <typename Go> void by_type(int32_t t, Go go) {
+  if (t == DMT_F32) go(Int<DMT_F32>());
+  else if (t == DMT_F16) go(Int<DMT_F16>());
+  else go(Int<DMT_BF16>());
+}
+
+constexpr int64_t kMost = (1ll << 31) - 1;
+bool few(int64_t n, int64_t k) { return k <= kMost && n <= kMost / std::max<int64_t>(k, 1); }
+int64_t stretch(int64_t m) {                       // of a wave: at most kTiles tiles of kSortWaves stretches
+  const int64_t per = (m + kTiles * kSortWaves - 1) / (kTiles * kSortWaves);
+  return std::max<int64_t>(256, (per + 63) / 64 * 64);
+}
+int64_t tiles(int64_t m) { return std::max<int64_t>(1, (m + kSortWaves * stretch(m) - 1) / (kSortWaves * stretch(m))); }
+
+}  // namespace
+
+extern "C" size_t dmt_expert_sort_workspace_bytes(int64_t n, int64_t k, int64_t num_experts) {
+  if (n < 0 || k < 1 || num_experts < 1 || num_experts > DMT_EXPERT_MAX || !few(n, k)) return 0;
+  return sizeof(int32_t) * (size_t)(tiles(n * k) > 1 ? tiles(n * k) * num_experts : 0);
+}
+
+extern "C" dmt_status dmt_expert_sort(const int32_t* experts, int64_t n, int64_t k, int64_t num_experts,
+                                      int64_t capacity, int32_t* slot, int32_t* source, int32_t* offsets,
+                                      int32_t* counts, int64_t* first_bad, void* workspace, size_t workspace_bytes,
+                                      void* stream) {
+  if (n < 0 || k < 1 || num_experts < 1 || capacity < 0) return DMT_EINVAL;
+  if (n > 0 && (!dmt_is_at(experts, 4) || !dmt_is_at(slot, 4))) return DMT_EINVAL;
+  if (!dmt_may_be_at(offsets, 4) || !dmt_may_be_at(counts, 4) || !dmt_may_be_at(first_bad, 8)) return DMT_EINVAL;
+  if (num_experts > DMT_EXPERT_MAX || !few(n, k) || capacity > kMost / num_experts) return DMT_ENOTSUP;
+  Sort a = {};
+  a.m = n * k, a.rows = capacity ? num_experts * capacity : a.m;
+  if (a.rows > 0 && !dmt_is_at(source, 4)) return DMT_EINVAL;
+  a.tiles = (int)tiles(a.m), a.stretch = stretch(a.m);
+  const size_t need = dmt_expert_sort_workspace_bytes(n, k, num_experts);
+  if (need > 0 && !dmt_is_at(workspace, 256)) return DMT_EINVAL;
+  if (workspace_bytes < need) return DMT_ENOMEM;
+  a.experts = experts, a.E = (int)num_experts, a.capacity = capacity;
+  while ((1 << a.bits) < a.E) ++a.bits;
+  a.slot = slot, a.source = source, a.offsets = offsets, a.counts = counts, a.part = (int32_t*)workspace;
+  a.first_bad = (unsigned long long*)first_bad;
+  hipStream_t s = (hipStream_t)stream;
+  const int lds = (int)sizeof(int) * ((kSortWaves + 2) * a.E + kSortWaves + 1);
+  static DmtPerDevice allowed;
+  dmt_allow_lds(allowed, (const void*)expert_place, (int)sizeof(int) * ((kSortWaves + 2) * DMT_EXPERT_MAX + kSortWaves + 1));
+  if (a.tiles > 1) hipLaunchKernelGGL(expert_count, dim3(a.tiles), dim3(kSortBlock), (unsigned)(sizeof(int) * a.E), s, a);
+  hipLaunchKernelGGL(expert_place, dim3(a.tiles), dim3(kSortBlock), lds, s, a);
+  return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
+}
+
+// Waves, one a row, four to a block.
+template <typename Kernel> static void by_rows(Kernel kernel, const Move& a, int64_t rows, hipStream_t s) {
+  dmt_launches((rows + kBlock / 64 - 1) / (kBlock / 64), kBlock,
+               [&](unsigned first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, a, first); });
+}
+
+extern "C" dmt_status dmt_expert_gather(const void* x, int64_t n, int64_t cols, int64_t x_stride, int32_t dtype,
+                                        const int32_t* slot, int64_t k, const int32_t* source, int64_t rows, void* out,
+                                        int64_t out_stride, void* stream) {
+  if (n < 0 || rows < 0 || cols < 1 || k < 1 || x_stride < cols || out_stride < cols || !dmt_is_dtype(dtype)) return DMT_EINVAL;
+  const int64_t e = dmt_ebytes(dtype);
+  if (n > 0 && (!dmt_is_at(x, e) || !dmt_is_at(slot, 4))) return DMT_EINVAL;
+  if (rows > 0 && (!dmt_is_at(out, e) || !dmt_is_at(source, 4))) return DMT_EINVAL;
+  if (!few(n, k) || rows > kMost || cols > 1 << 24) return DMT_ENOTSUP;
+  if (rows == 0) return DMT_OK;
+  Move a = {};
+  a.x = (const char*)x, a.out = (char*)out, a.x_stride = x_stride, a.out_stride = out_stride, a.n = n, a.rows = rows;
+  a.slot = slot, a.source = source, a.cols = (int)cols, a.k = (int)k;
+  if (dtype == DMT_F32) by_rows(expert_gather<4>, a, rows, (hipStream_t)stream);
+  else by_rows(expert_gather<2>, a, rows, (hipStream_t)stream);
+  return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
+}
+
+extern "C" dmt_status dmt_expert_combine(const void* z, int64_t rows, int64_t cols, int64_t z_stride, int32_t dtype,
+                                         const int32_t* slot, int64_t n, int64_t k, const float* weights, void* y,
+                                         int64_t y_stride, int32_t y_dtype, void* stream) {
+  if (n < 0 || rows < 0 || cols < 1 || k < 1 || z_stride < cols || y_stride < cols || !dmt_is_dtype(dtype) || !dmt_is_dtype(y_dtype))
+    return DMT_EINVAL;
+  if (rows > 0 && !dmt_is_at(z, dmt_ebytes(dtype))) return DMT_EINVAL;
+  if (n > 0 && (!dmt_is_at(y, dmt_ebytes(y_dtype)) || !dmt_is_at(slot, 4))) return DMT_EINVAL;
+  if (!dmt_may_be_at(weights, 4)) return DMT_EINVAL;
+  if (!few(n, k) || rows > kMost || cols > 1 << 24) return DMT_ENOTSUP;
+  if (n == 0) return DMT_OK;
+  Move a = {};
+  a.z = (const char*)z, a.out = (char*)y, a.z_stride = z_stride, a.out_stride = y_stride, a.n = n, a.rows = rows;
+  a.slot = slot, a.weights = weights, a.cols = (int)cols, a.k = (int)k;
+  by_type(dtype, [&](auto d) {
+    by_type(y_dtype, [&](auto o) { by_rows(expert_combine<decltype(d)::value, decltype(o)::value>, a, n, (hipStream_t)stream); });
+  });
+  return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
+}
+
+extern "C" dmt_status dmt_expert_combine_bwd(const void* dy, int64_t n, int64_t cols, int64_t dy_stride,
+                                             int32_t grad_dtype, const void* z, int64_t rows, int64_t z_stride,
+                                             int32_t dtype, const int32_t* slot, int64_t k, const int32_t* source,
+                                             const float* weights, void* dz, int64_t dz_stride, float* dweights,
+                                             void* stream) {
+  if (n < 0 || rows < 0 || cols < 1 || k < 1 || dy_stride < cols || !dmt_is_dtype(dtype)) return DMT_EINVAL;
+  if (grad_dtype != dtype && grad_dtype != DMT_F32) return DMT_EINVAL;
+  const int64_t ge = dmt_ebytes(grad_dtype);
+  if (n > 0 && (!dmt_is_at(dy, ge) || !dmt_is_at(slot, 4))) return DMT_EINVAL;
+  if (dz && (dz_stride < cols || !dmt_is_at(dz, ge) || (rows > 0 && !dmt_is_at(source, 4)))) return DMT_EINVAL;
+  if (dweights && (z_stride < cols || !dmt_is_at(dweights, 4) || (rows > 0 && !dmt_is_at(z, dmt_ebytes(dtype))))) return DMT_EINVAL;
+  if (!dmt_may_be_at(weights, 4)) return DMT_EINVAL;
+  if (!few(n, k) || rows > kMost || cols > 1 << 24) return DMT_ENOTSUP;
+  if (n == 0 && (!dz || rows == 0)) return DMT_OK;
+  Move a = {};
+  a.x = (const char*)dy, a.z = (const char*)z, a.out = (char*)dz, a.x_stride = dy_stride, a.z_stride = z_stride;
+  a.out_stride = dz_stride, a.n = n, a.rows = rows, a.slot = slot, a.source = source, a.weights = weights;
+  a.dweights = dweights, a.cols = (int)cols, a.k = (int)k;
+  hipStream_t s = (hipStream_t)stream;
+  if (dz && rows > 0) {
+    if (grad_dtype == DMT_F32) by_rows(expert_clear<4>, a, rows, s);
+    else by_rows(expert_clear<2>, a, rows, s);
+  }
+  if (n > 0 && (dz || dweights))
+    by_type(dtype, [&](auto d) {
+      constexpr int D = decltype(d)::value;
+      if (grad_dtype == D) by_rows(expert_combine_bwd<D, D>, a, n, s);
+      else by_rows(expert_combine_bwd<D, DMT_F32>, a, n, s);
+    });
+  return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
+}
