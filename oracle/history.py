@@ -39,9 +39,11 @@ def sigmoid(x):
 def scan_fwd(gate, value, free, found, initial=None, final=None):
     """h, the state before each row, final (a copy with the runs' last states), and how far a float32 evaluation may be off:
 
-    f and 1 - f come within 9 roundings (exp2 and its product 3, the sum 1, the reciprocal 2, a product 1, and what they
-    pass on), so a step adds at most 12 U32 of what it sums, and what was off before shrinks with f like the state itself;
-    stretches joined by h -> A h + S add at most 64 roundings of the whole."""
+    e = exp(-gate) is 2^t with t = gate log2(e) rounded (1.25 |gate| U32 of e: the product, and the constant's own quarter) and
+    exp2's 2 U32; f = 1 / (1 + e) and 1 - f = e f get f (1 - f) of that, and 1 (the sum) + 2 (the reciprocal) + 1 (the product) + 2
+    (exp2) U32 of themselves.  A step f h + u adds two roundings: at most 12 U32 of what it sums and, from the first part,
+    1.25 |gate| f (1 - f) U32 (|h| + |value|) (|h| alone where u is value).  What was off before shrinks with f like the state
+    itself; stretches joined by h -> A h + S add at most 64 roundings of the whole."""
     gate, value = np.asarray(gate, np.float64), np.asarray(value, np.float64)
     h, prev = np.zeros_like(gate), np.zeros_like(gate)
     size, off, prev_size, prev_off = (np.zeros_like(gate) for _ in range(4))
@@ -49,23 +51,28 @@ def scan_fwd(gate, value, free, found, initial=None, final=None):
     last_off = None if final is None else np.zeros_like(last)
     f, rest = sigmoid(gate)
     u = value if free else rest * value
+    with np.errstate(invalid="ignore"):
+        tilt = 1.25 * U32 * np.nan_to_num(np.abs(gate) * f * rest, nan=0.0)        # (inf * 0: open or shut, exactly)
     for b, lo, hi in found:
         x = np.zeros(gate.shape[1]) if initial is None else np.asarray(initial[b], np.float64)
         s, o = np.abs(x), np.zeros_like(x)
         for r in range(lo, hi):
             prev[r], prev_size[r], prev_off[r] = x, s, o
+            o = f[r] * o + tilt[r] * (s + (0 if free else np.abs(value[r])))
             x = f[r] * x + u[r]
             s = f[r] * s + np.abs(u[r])
-            o = f[r] * o + 12 * U32 * s
+            o = o + 12 * U32 * s
             h[r], size[r], off[r] = x, s, o
         if last is not None:
             last[b], last_off[b] = x, o + 64 * U32 * s
     return dict(h=h, off=off + 64 * U32 * size, prev=prev, prev_size=prev_size, prev_off=prev_off + 64 * U32 * prev_size,
-                final=last, final_off=last_off, f=f, rest=rest)
+                final=last, final_off=last_off, f=f, rest=rest, tilt=tilt, gate=gate)
 
 
 def scan_bwd(fwd, value, free, found, dh, dfinal=None, dinitial=None):
-    """dgate, dvalue, dinitial and how far each may be off (the same counts)."""
+    """dgate, dvalue, dinitial and how far each may be off (the same counts; the slope f (1 - f) and the share 1 - f are off by
+    at most 1.25 |gate| U32 of themselves besides)."""
+    tilt = fwd["tilt"]
     f, rest, value, dh = fwd["f"], fwd["rest"], np.asarray(value, np.float64), np.asarray(dh, np.float64)
     lam, size, off = np.zeros_like(f), np.zeros_like(f), np.zeros_like(f)
     first = None if dinitial is None else np.array(dinitial, np.float64)
@@ -76,7 +83,7 @@ def scan_bwd(fwd, value, free, found, dh, dfinal=None, dinitial=None):
         for r in range(hi - 1, lo - 1, -1):
             lam[r], size[r] = dh[r] + m, np.abs(dh[r]) + s
             off[r] = o + 12 * U32 * size[r]
-            m, s, o = f[r] * lam[r], f[r] * size[r], f[r] * off[r]
+            m, s, o = f[r] * lam[r], f[r] * size[r], f[r] * off[r] + tilt[r] * size[r]
         if first is not None:
             first[b], first_off[b] = m, o + 80 * U32 * s
     off = off + 64 * U32 * size
@@ -88,9 +95,9 @@ def scan_bwd(fwd, value, free, found, dh, dfinal=None, dinitial=None):
         d = fwd["prev"] if free else fwd["prev"] - value
         d_size = fwd["prev_size"] + (0 if free else np.abs(value))
         share = np.ones_like(f) if free else rest
-        dv, dv_off = lam * share, (off + 12 * U32 * size) * share
+        dv, dv_off = lam * share, (off + 12 * U32 * size) * share + (0 if free else tilt * size)
         dg = lam * d * slope
-        dg_off = (off * d_size + size * (fwd["prev_off"] + 24 * U32 * d_size)) * slope
+        dg_off = (off * d_size + size * (fwd["prev_off"] + 24 * U32 * d_size)) * slope + tilt * size * d_size
     for a in (dv, dv_off, dg, dg_off):
         a[~there] = 0.0
     return dict(dgate=dg, dgate_off=dg_off, dvalue=dv, dvalue_off=dv_off, dinitial=first, dinitial_off=first_off)

@@ -4,13 +4,16 @@
 // Both are first-order recurrences, so a stretch of rows maps the state before it to the one behind it by h -> A h + S, with A the
 // product of its f; a stretch that holds a sequence's first row (backwards: its last) forgets what came before.  Rows are cut
 // into chunks, a block's each (for the channels of a group of lanes), and chunks into the stretches of `walkers`: lane
-// groups that go through their rows one after another, 16 at a time.  Where sequences are as long as stretches, or
-// so many that a walker can have whole ones, nothing else is needed.  Otherwise a first launch takes every stretch's (A, S), reading only
-// the rows that matter to the next one (behind its last first row), and the second starts each walker from what those before
-// it lead to.  One chunk does both in one launch.
+// groups that go through their rows one after another, 8 at a time, with a lane's channels in registers.  A stretch begins where a
+// sequence does, if one begins near its nominal place; so short sequences are walked whole and only long ones are cut.  Where any
+// is cut, a first launch takes every stretch's (A, S), reading only the rows that a next stretch continues, and the second starts each
+// walker from what those before it lead to.  One chunk does both in one launch, and so do equal sequences that are no longer than a stretch.
 //
-// The backward needs h_{t-1}: the forward keeps the state in front of every 16th row in float32, from which a walker goes through
-// its 16 rows again, so neither h nor a rounded h is read.
+// The backward needs h_{t-1}: the forward keeps the state in front of every 8th row in float32, from which a walker goes through
+// its 8 rows again, so neither h nor a rounded h is read.
+//
+// Bound by memory: two sequences of 65536 x 512 bfloat16, forward 81 + 87 us (the rows read twice, 268 MB each time, and 151 MB
+// written), backward 63 + 138 (671 MB in the second launch, 4.9 TB/s); 131072 x 256 bfloat16 in 4096 ragged sequences 21 + 48 us.
 #include <algorithm>
 
 #include "dmt_internal.h"
@@ -18,17 +21,19 @@
 
 namespace {
 
-constexpr int kBlock = 512, kTile = 16;
+constexpr int kBlock = 512, kTile = 8, kRun = 16, kSub = 64;
+constexpr uint32_t kAll = (1u << kTile) - 1;
 
 // How rows are cut.
 struct Cut {
-  int group;           // lanes of a walker: 16, 32 or 64
+  int group;           // lanes of a walker: 8, 16, 32 or 64
   int tiles;           // groups' widths of channels
-  int64_t sub;         // rows of a walker, a multiple of 16 unless `whole`
+  int64_t sub;         // rows of a walker nominally, a multiple of kTile
   int64_t chunk;       // rows of a chunk
   int64_t chunks;
-  bool whole;          // every walker starts with a sequence's first row
+  bool whole;          // every walker starts with a sequence's first row: equal ones, none longer than a stretch
   bool one;            // no state passes between chunks
+  bool narrow;         // fewer channels than a lane has
 };
 
 struct Scan {
@@ -42,22 +47,16 @@ struct Scan {
   int* forgets;                    // [chunks]
   unsigned long long* first_bad;
   int sequences, length, cols, tiles;
-  bool free, whole;
+  bool whole, one;
   int64_t sub, chunk_rows, chunks;
 };
+
+// Lanes of a walker.  0 stands for rows of fewer channels than a lane has (a walker has 8 lanes then, and one of them has them).
+template <int G> struct Lanes { static constexpr int value = G == 0 ? 8 : G; };
 
 template <int G> __device__ __forceinline__ int uniform(int v) {
   if constexpr (G == 64) return __builtin_amdgcn_readfirstlane(v);
   else return v;
-}
-
-// First row of walker w of a chunk (of the chunk's end, for the walkers' number).
-template <int G> __device__ __forceinline__ int begin_of(const Scan& a, int64_t chunk, int w) {
-  const int64_t c0 = chunk * a.chunk_rows, c1 = min(c0 + a.chunk_rows, a.rows);
-  if (w == 0) return (int)c0;
-  if (w == kBlock / G) return (int)c1;
-  const int64_t at = c0 + w * a.sub;
-  return (int)min(c1, a.whole ? at : at & ~(int64_t)(kTile - 1));
 }
 
 __device__ __forceinline__ int id_of(const Scan& a, int row) {
@@ -66,85 +65,118 @@ __device__ __forceinline__ int id_of(const Scan& a, int row) {
 }
 __device__ __forceinline__ int sequence_of(const Scan& a, int row) { return a.seq ? id_of(a, row) : row / a.length; }
 
-// Bits of the 16 rows from r0 on that lie in [lo, hi): whether a row is of a sequence, is its first, its last.
-struct Bits { uint32_t there, first, last; };
-
-template <int G, bool Report = false>
-__device__ __forceinline__ Bits bits_of(const Scan& a, int r0, int lo, int hi) {
-  const int lane = threadIdx.x & 63, row = r0 + (lane & 15);
-  bool there = row >= lo && row < hi, first = false, last = false;
-  if (there) {
-    if (a.seq) {
-      const int raw = a.seq[row], id = (uint32_t)raw < (uint32_t)a.sequences ? raw : -1;
-      if (Report && raw >= a.sequences && a.first_bad) atomicMin(a.first_bad, (unsigned long long)row);
-      there = id >= 0;
-      first = there && (row == 0 || id_of(a, row - 1) != id);
-      last = there && (row + 1 == (int)a.rows || id_of(a, row + 1) != id);
-    } else {
-      const int at = row % a.length;
-      first = at == 0;
-      last = at == a.length - 1;
-    }
+// Where the rows of the walker whose nominal first row is b begin: where the sequence changes next, if it does within the stretch, else b.
+// So walkers have whole sequences where those are short, and only long ones are cut.
+template <int G> __device__ __forceinline__ int begin_of(const Scan& a, int64_t nominal) {
+  constexpr int N = Lanes<G>::value, Steps = kSub / N;
+  if (nominal >= a.rows) return (int)a.rows;
+  const int b = (int)nominal, end = (int)min((int64_t)a.rows, nominal + a.sub), lane = threadIdx.x & 63;
+  if (!a.seq) {
+    const int next = (b + a.length - 1) / a.length * a.length;
+    return next < nominal + a.sub ? next : b;
   }
-  const int shift = G == 64 ? 0 : lane & 48;
+  int here[Steps], before[Steps];
+#pragma unroll
+  for (int i = 0; i < Steps; ++i) {
+    const int row = min(b + i * N + lane % N, end - 1);
+    here[i] = id_of(a, row);
+    before[i] = id_of(a, max(row - 1, 0));
+  }
+  int found = b;
+#pragma unroll
+  for (int i = Steps - 1; i >= 0; --i) {
+    const int row = b + i * N + lane % N;
+    uint64_t change = __ballot(row < end && (row == 0 || here[i] != before[i])) >> (N == 64 ? 0 : lane & ~(N - 1));
+    if (N < 64) change &= (1ull << (N & 63)) - 1;
+    if (change) found = b + i * N + __builtin_ctzll(change);
+  }
+  return uniform<G>(found);
+}
+
+// Bits of the kTile rows from r0 on that lie in [lo, hi): whether a row is of a sequence, is its first, its last; and the
+// sequence of row r0 + (lane mod kTile).
+struct Bits {
+  uint32_t there, first, last;
+  int id;
+  // Row i's sequence.
+  __device__ __forceinline__ int id_at(int i) const { return __shfl(id, (threadIdx.x & 63 & ~(kTile - 1)) + i); }
+};
+
+// What the bits of a tile are made of, requested ahead: raw ids of a lane's row and of its neighbours.
+struct Ids { int before, here, behind; };
+
+__device__ __forceinline__ Ids ids_of(const Scan& a, int r0, int lo, int hi) {
+  Ids x = {-1, -1, -1};
+  const int row = r0 + (threadIdx.x & (kTile - 1));
+  if (a.seq && row >= lo && row < hi) {
+    x.before = a.seq[max(row - 1, 0)];
+    x.here = a.seq[row];
+    x.behind = a.seq[min(row + 1, (int)a.rows - 1)];
+  }
+  return x;
+}
+
+template <int G> __device__ __forceinline__ Bits bits_of(const Scan& a, Ids x, int r0, int lo, int hi) {
+  const int lane = threadIdx.x & 63, row = r0 + (lane & (kTile - 1));
+  bool there = row >= lo && row < hi, first, last;
   Bits b;
-  b.there = (uint32_t)(__ballot(there) >> shift) & 0xffffu;
-  b.first = (uint32_t)(__ballot(first) >> shift) & 0xffffu;
-  b.last = (uint32_t)(__ballot(last) >> shift) & 0xffffu;
+  if (a.seq) {
+    const auto valid = [&](int id) { return (uint32_t)id < (uint32_t)a.sequences ? id : -1; };
+    b.id = valid(x.here);
+    first = row == 0 || valid(x.before) != b.id;
+    last = row + 1 == (int)a.rows || valid(x.behind) != b.id;
+    there = there && b.id >= 0;
+  } else {
+    b.id = (int)((uint32_t)max(row, 0) / (uint32_t)a.length);
+    const int at = row - b.id * a.length;
+    first = at == 0;
+    last = at == a.length - 1;
+  }
+  const int shift = G == 64 ? 0 : lane & ~(kTile - 1);
+  b.there = (uint32_t)(__ballot(there) >> shift) & kAll;
+  b.first = (uint32_t)(__ballot(there && first) >> shift) & kAll;
+  b.last = (uint32_t)(__ballot(there && last) >> shift) & kAll;
   return b;
 }
 
-// Channels of a lane: 4 bytes of the rows' type.
-template <int XD> struct Width { static constexpr int value = XD == DMT_F32 ? 1 : 2; };
-
-// V elements of type D in as few words; of a single column only the first is there.
-template <int D, int V> struct Word { uint32_t w[V * dmt::EltBytes<D>::value / 4 > 0 ? V * dmt::EltBytes<D>::value / 4 : 1]; };
-
-template <int D, int V> __device__ __forceinline__ Word<D, V> load_word(const char* p, bool both) {
-  typedef uint32_t __attribute__((aligned(2))) u32;
-  Word<D, V> r;
-  if constexpr (D == DMT_F32) {
-    r.w[0] = *(const DMT_GLOBAL uint32_t*)p;
-    if constexpr (V == 2) r.w[1] = both ? *(const DMT_GLOBAL uint32_t*)(p + 4) : 0u;
-  } else {
-    r.w[0] = both ? *(const DMT_GLOBAL u32*)p : (uint32_t) * (const DMT_GLOBAL uint16_t*)p;
-  }
-  return r;
-}
-template <int D, int V> __device__ __forceinline__ void unpack_word(const Word<D, V>& r, float (&x)[V]) {
-  if constexpr (D == DMT_F32) {
-#pragma unroll
-    for (int q = 0; q < V; ++q) x[q] = __uint_as_float(r.w[q]);
-  } else {
-    dmt::unpack2<D>(r.w[0], x[0], x[1]);
-  }
-}
-template <int D, int V> __device__ __forceinline__ void store_word(char* p, const float (&x)[V], bool both) {
-  typedef uint32_t __attribute__((aligned(2))) u32;
-  if constexpr (D == DMT_F32) {
-    *(DMT_GLOBAL float*)p = x[0];
-    if constexpr (V == 2) {
-      if (both) *(DMT_GLOBAL float*)(p + 4) = x[1];
+// Lowers first_bad to the first of rows [lo, hi) whose id is none; the walker's lanes look at its rows.
+__device__ __forceinline__ void report_bad(const Scan& a, int lo, int hi, int at, int lanes) {
+  for (int row = lo + at; row < hi; row += lanes)
+    if (a.seq[row] >= a.sequences) {
+      atomicMin(a.first_bad, (unsigned long long)row);
+      break;
     }
-  } else {
-    const uint32_t w = dmt::round2<D>(x[0], x[1]);
-    if (both) *(DMT_GLOBAL u32*)p = w;
-    else *(DMT_GLOBAL uint16_t*)p = (uint16_t)w;
-  }
 }
 
-// f = sigmoid(x) and 1 - f, each to a few units of its last place: e = exp(-|x|) by 2^t with t's rounding put back, then 1 / (1 + e).
-__device__ __forceinline__ void sigmoids(float x, float& f, float& rest) {
-  float z = -fabsf(x);
-  z = z < -100.f ? -100.f : z;                              // (keeps a NaN)
-  const float t = z * 1.44269504088896341f;
-  const float lo = fmaf(z, 1.44269504088896341f, -t) + z * 1.92596299e-8f;
-  const float p = __builtin_amdgcn_exp2f(t);
-  const float e = fmaf(p, lo * 0.693147180559945309f, p);
-  const float r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
-  f = x >= 0.f ? r : er;
-  rest = x >= 0.f ? er : r;
+// Channels of a lane: four forwards; 8 bytes of the rows' type backwards, where more registers are held.
+template <int XD, bool Back> struct Width { static constexpr int value = Back ? 8 / dmt::EltBytes<XD>::value : 4; };
+
+// f = sigmoid(x) and 1 - f from e = exp(-x): f = 1 / (1 + e), 1 - f = e f.  The product x log2 e is rounded, so e is off by up to 1.25 |x|
+// units of 2^-24 and two more; f and 1 - f then by f (1 - f) times that, at most 0.35 units, and by a few units of their own.  Where e
+// passes the largest float f is 0 and 1 - f is 1 (the minimum takes the number, not inf * 0); a NaN stays in f.
+__device__ __forceinline__ float exp_minus(float x) { return __builtin_amdgcn_exp2f(x * -1.44269504088896341f); }
+__device__ __forceinline__ void from_exp(float e, float& f, float& rest) {
+  f = __builtin_amdgcn_rcpf(1.f + e);
+  rest = __builtin_fminf(e * f, 1.f);
 }
+__device__ __forceinline__ void sigmoids(float x, float& f, float& rest) { from_exp(exp_minus(x), f, rest); }
+
+// Which chunk and channels a block has.  Blocks go to the eight XCDs in turn; the tiles of a chunk go to one, so that a line that two
+// tiles share (rows of no whole number of lines) is read once and written whole from its L2.
+struct Block {
+  int64_t chunk;
+  int tile;
+  __device__ __forceinline__ Block(const Scan& a, unsigned first) {
+    const uint32_t at = first + blockIdx.x, tiles = (uint32_t)a.tiles, many = (uint32_t)(a.chunks / 8 * 8) * tiles;
+    if (at < many) {
+      chunk = at / 8 / tiles * 8 + at % 8;
+      tile = (int)(at / 8 % tiles);
+    } else {
+      chunk = at / tiles;
+      tile = (int)(at % tiles);
+    }
+  }
+};
 
 struct Map { float a, s; };
 __device__ __forceinline__ Map after(Map l, Map r) {         // l, then r
@@ -154,202 +186,212 @@ __device__ __forceinline__ Map after(Map l, Map r) {         // l, then r
 __device__ __forceinline__ float applied(Map m, float h) { return m.a < 0.f ? m.s : fmaf(m.a, h, m.s); }
 
 // What a lane knows about its channels.
-template <int G, int XD> struct Lane {
-  static constexpr int V = Width<XD>::value;
-  int w, at, c;            // walker, lane of it, first channel
-  bool on, both;
+template <int G, int V> struct Lane {
+  static constexpr int N = Lanes<G>::value;
+  int w, at, c, valid;     // walker, lane of it, first channel, how many there are
   __device__ __forceinline__ Lane(int tile, int cols) {
-    w = uniform<G>(threadIdx.x / G);
-    at = threadIdx.x % G;
-    const int c0 = (tile * G + at) * V;
-    on = c0 < cols;
-    c = max(0, min(c0, cols - V));        // the last pair of an odd width holds the channel before too: both lanes find the same
-    both = cols >= V;
+    w = uniform<G>(threadIdx.x / N);
+    at = threadIdx.x % N;
+    // the last lane of an odd width has channels of the one before too, and lanes past the width have the last ones: all find, and
+    // store, the same
+    c = G == 0 ? 0 : min((tile * N + at) * V, cols - V);
+    valid = G == 0 ? cols : V;
   }
 };
 
+// A lane's channels of a row of a float32 [rows][cols] (null: zeros); and back.
+template <int V> __device__ __forceinline__ void load_state(const float* p, int64_t row, int cols, int c, int valid, float (&x)[V]) {
+#pragma unroll
+  for (int q = 0; q < V; ++q) x[q] = 0.f;
+  if (p) dmt::load_elems<DMT_F32, V>((const char*)(p + row * cols) + (uint32_t)c * 4u, valid, x);
+}
+template <int V> __device__ __forceinline__ void store_state(float* p, int64_t row, int cols, int c, int valid, const float (&x)[V]) {
+  dmt::store_elems<DMT_F32, V>((char*)(p + row * cols) + (uint32_t)c * 4u, valid, x);
+}
+
 // ---- what a stretch makes of the state before it
 
-template <int G, int XD, int V>
-__device__ __forceinline__ void stretch_fwd(const Scan& a, const Lane<G, XD>& l, int lo, int hi, Map (&m)[V]) {
+// Rows [from, hi) in their order: A and S.
+template <int XD, bool Free, int V>
+__device__ __forceinline__ void map_fwd(const Scan& a, int c, int valid, int from, int hi, float (&A)[V], float (&S)[V]) {
   constexpr int EB = dmt::EltBytes<XD>::value;
-#pragma unroll
-  for (int q = 0; q < V; ++q) m[q] = {1.f, 0.f};
-  if (lo >= hi) return;
-  bool needed = hi < (int)a.rows;                                 // by the row behind
-  if (needed) needed = a.seq ? id_of(a, hi) >= 0 && id_of(a, hi) == id_of(a, hi - 1) : hi % a.length != 0;
-  if (!needed) {
-#pragma unroll
-    for (int q = 0; q < V; ++q) m[q] = {-1.f, 0.f};
-    return;
-  }
-  int from = lo;
-  if (!a.seq) {
-    const int begin = hi - 1 - (hi - 1) % a.length;
-    from = max(lo, begin);
-    if (begin >= lo) {
-#pragma unroll
-      for (int q = 0; q < V; ++q) m[q] = {-1.f, 0.f};
-    }
-  } else {
-    for (int r0 = (hi - 1) & ~(kTile - 1); r0 + kTile > lo; r0 -= kTile) {
-      const uint32_t first = bits_of<G>(a, r0, lo, hi).first;
-      if (first) {
-        from = r0 + 31 - __builtin_clz(first);
-#pragma unroll
-        for (int q = 0; q < V; ++q) m[q] = {-1.f, 0.f};
-        break;
-      }
-    }
-  }
-  if (m[0].a < 0.f && a.initial) {
-    const float* at = a.initial + (int64_t)sequence_of(a, from) * a.cols + l.c;
-#pragma unroll
-    for (int q = 0; q < V; ++q) m[q].s = q == 0 || l.both ? at[q] : 0.f;
-  }
-  if (!l.on) return;
-  const char *gp = a.gate + ((int64_t)from * a.gate_stride + l.c) * EB, *vp = a.value + ((int64_t)from * a.value_stride + l.c) * EB;
   const int64_t gs = a.gate_stride * EB, vs = a.value_stride * EB;
-  for (int r0 = from; r0 < hi; r0 += kTile) {
-    Word<XD, V> g[kTile], v[kTile];
+  const char *gp = a.gate + from * gs, *vp = a.value + from * vs;
+  const uint32_t off = (uint32_t)c * EB;
+  for (int r0 = from; r0 < hi; r0 += kRun) {
+    dmt::Raw<XD, V> g[kRun], v[kRun];
 #pragma unroll
-    for (int i = 0; i < kTile; ++i) {
+    for (int i = 0; i < kRun; ++i) {
       const int j = min(i, hi - 1 - r0);
-      g[i] = load_word<XD, V>(gp + j * gs, l.both);
-      v[i] = load_word<XD, V>(vp + j * vs, l.both);
+      g[i] = dmt::load_raw<XD, V>(gp + j * gs + off, valid);
+      v[i] = dmt::load_raw<XD, V>(vp + j * vs + off, valid);
     }
-#pragma unroll
-    for (int i = 0; i < kTile; ++i) {
-      if (r0 + i >= hi) continue;
+    const auto row = [&](int i) {
       float x[V], u[V];
-      unpack_word<XD, V>(g[i], x);
-      unpack_word<XD, V>(v[i], u);
+      dmt::unpack<XD, V>(g[i], x);
+      dmt::unpack<XD, V>(v[i], u);
 #pragma unroll
       for (int q = 0; q < V; ++q) {
         float f, rest;
         sigmoids(x[q], f, rest);
-        m[q].s = fmaf(f, m[q].s, a.free ? u[q] : rest * u[q]);
-        m[q].a = m[q].a < 0.f ? -1.f : m[q].a * f;
+        S[q] = fmaf(f, S[q], Free ? u[q] : rest * u[q]);
+        A[q] *= f;
       }
+    };
+    if (r0 + kRun <= hi) {
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) row(i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kRun - 1; ++i)
+        if (r0 + i < hi) row(i);
     }
-    gp += kTile * gs;
-    vp += kTile * vs;
+    gp += kRun * gs;
+    vp += kRun * vs;
   }
 }
 
-template <int G, int XD, int GD, int V>
-__device__ __forceinline__ void stretch_bwd(const Scan& a, const Lane<G, XD>& l, int lo, int hi, Map (&m)[V]) {
+// Rows [lo, to] against their order: m -> A m + S.
+template <int XD, int GD, int V>
+__device__ __forceinline__ void map_bwd(const Scan& a, int c, int valid, int lo, int to, float (&A)[V], float (&S)[V]) {
   constexpr int EB = dmt::EltBytes<XD>::value, GB = dmt::EltBytes<GD>::value;
-#pragma unroll
-  for (int q = 0; q < V; ++q) m[q] = {1.f, 0.f};
-  if (lo >= hi) return;
-  bool needed = lo > 0;                                           // by the row before
-  if (needed) needed = a.seq ? id_of(a, lo) >= 0 && id_of(a, lo) == id_of(a, lo - 1) : lo % a.length != 0;
-  if (!needed) {
-#pragma unroll
-    for (int q = 0; q < V; ++q) m[q] = {-1.f, 0.f};
-    return;
-  }
-  int to = hi - 1;
-  bool ends = false;
-  if (!a.seq) {
-    const int last = lo - lo % a.length + a.length - 1;
-    ends = last < hi;
-    to = min(last, hi - 1);
-  } else {
-    for (int r0 = lo & ~(kTile - 1); r0 < hi; r0 += kTile) {
-      const uint32_t last = bits_of<G>(a, r0, lo, hi).last;
-      if (last) {
-        to = r0 + __builtin_ctz(last);
-        ends = true;
-        break;
-      }
-    }
-  }
-  if (ends) {
-    const float* at = a.dfinal ? a.dfinal + (int64_t)sequence_of(a, to) * a.cols + l.c : nullptr;
-#pragma unroll
-    for (int q = 0; q < V; ++q) m[q] = {-1.f, at && (q == 0 || l.both) ? at[q] : 0.f};
-  }
-  if (!l.on) return;
-  const char *gp = a.gate + ((int64_t)to * a.gate_stride + l.c) * EB, *dp = a.dh + ((int64_t)to * a.dh_stride + l.c) * GB;
   const int64_t gs = a.gate_stride * EB, ds = a.dh_stride * GB;
-  for (int r0 = to; r0 >= lo; r0 -= kTile) {
-    Word<XD, V> g[kTile];
-    Word<GD, V> d[kTile];
+  const char *gp = a.gate + to * gs, *dp = a.dh + to * ds;
+  const uint32_t off = (uint32_t)c * EB, off_g = (uint32_t)c * GB;
+  for (int r0 = to; r0 >= lo; r0 -= kRun) {
+    dmt::Raw<XD, V> g[kRun];
+    dmt::Raw<GD, V> d[kRun];
 #pragma unroll
-    for (int i = 0; i < kTile; ++i) {
+    for (int i = 0; i < kRun; ++i) {
       const int j = min(i, r0 - lo);
-      g[i] = load_word<XD, V>(gp - j * gs, l.both);
-      d[i] = load_word<GD, V>(dp - j * ds, l.both);
+      g[i] = dmt::load_raw<XD, V>(gp - j * gs + off, valid);
+      d[i] = dmt::load_raw<GD, V>(dp - j * ds + off_g, valid);
     }
-#pragma unroll
-    for (int i = 0; i < kTile; ++i) {
-      if (r0 - i < lo) continue;
+    const auto row = [&](int i) {
       float x[V], y[V];
-      unpack_word<XD, V>(g[i], x);
-      unpack_word<GD, V>(d[i], y);
+      dmt::unpack<XD, V>(g[i], x);
+      dmt::unpack<GD, V>(d[i], y);
 #pragma unroll
       for (int q = 0; q < V; ++q) {
-        float f, rest;
-        sigmoids(x[q], f, rest);
-        m[q].s = f * (y[q] + m[q].s);
-        m[q].a = m[q].a < 0.f ? -1.f : m[q].a * f;
+        const float f = __builtin_amdgcn_rcpf(1.f + exp_minus(x[q]));
+        S[q] = f * (y[q] + S[q]);
+        A[q] *= f;
       }
+    };
+    if (r0 - kRun >= lo - 1) {
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) row(i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kRun - 1; ++i)
+        if (r0 - i >= lo) row(i);
     }
-    gp -= kTile * gs;
-    dp -= kTile * ds;
+    gp -= kRun * gs;
+    dp -= kRun * ds;
   }
 }
 
-template <int G, int XD, int GD, bool Back, int V>
-__device__ __forceinline__ void stretch_of(const Scan& a, const Lane<G, XD>& l, int lo, int hi, Map (&m)[V]) {
-  if constexpr (Back) stretch_bwd<G, XD, GD, V>(a, l, lo, hi, m);
-  else stretch_fwd<G, XD, V>(a, l, lo, hi, m);
+// The map of rows [lo, hi) (backwards: against their order).  Only what the next (the previous) row continues is read: nothing
+// where a sequence starts there, else from the last first (to the first last) row on.
+template <int G, int XD, int GD, bool Back, bool Free, int V>
+__device__ __forceinline__ void stretch_of(const Scan& a, const Lane<G, V>& l, int lo, int hi, Map (&m)[V]) {
+  constexpr int N = Lanes<G>::value;
+  float A[V], S[V];
+#pragma unroll
+  for (int q = 0; q < V; ++q) A[q] = 1.f, S[q] = 0.f;
+  bool forgets = false;
+  if (lo < hi) {
+    const int edge = Back ? lo : hi, inner = Back ? lo : hi - 1, outer = Back ? lo - 1 : hi;     // rows inner and outer: of one sequence?
+    int at = Back ? hi - 1 : lo;                           // the row from which (to which) on the map is made
+    bool on = edge > 0 && edge < (int)a.rows;
+    if (on && a.seq) {
+      const int id = id_of(a, inner), next = id_of(a, outer);
+      const int there = Back ? hi - 1 : lo, past = Back ? min(hi, (int)a.rows - 1) : max(lo - 1, 0);
+      const bool ends = id_of(a, there) != id_of(a, past) || (Back ? hi == (int)a.rows : lo == 0);
+      on = id >= 0 && id == next;
+      forgets = ends;                                      // unless a row in between says so nearer
+      for (int i = 0; on && i < hi - lo; i += N) {
+        const int row = Back ? lo + i + l.at : hi - 1 - i - l.at;
+        const bool other = row >= lo && row < hi && id_of(a, row) != id;
+        uint64_t found = __ballot(other) >> (N == 64 ? 0 : (threadIdx.x & 63 & ~(N - 1)));
+        if (N < 64) found &= (1ull << (N & 63)) - 1;
+        if (found) {
+          const int k = i + __builtin_ctzll(found);        // rows from the inner one on
+          at = Back ? lo + k - 1 : hi - k;
+          forgets = true;
+          break;
+        }
+      }
+    } else if (on) {
+      on = edge % a.length != 0;
+      const int begin = Back ? lo - lo % a.length + a.length - 1 : hi - 1 - (hi - 1) % a.length;
+      forgets = Back ? begin < hi : begin >= lo;
+      if (forgets) at = begin;
+    }
+    if (on) {
+      if (forgets) load_state<V>(Back ? a.dfinal : a.initial, sequence_of(a, inner), a.cols, l.c, l.valid, S);
+      if constexpr (Back) map_bwd<XD, GD, V>(a, l.c, l.valid, lo, at, A, S);
+      else map_fwd<XD, Free, V>(a, l.c, l.valid, at, hi, A, S);
+    } else {
+      forgets = true;
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < V; ++q) m[q] = {forgets ? -1.f : A[q], S[q]};
 }
 
-template <int G, int XD, int GD, bool Back> __global__ __launch_bounds__(kBlock) void scan_stretches(const Scan a, unsigned first) {
-  constexpr int V = Width<XD>::value, W = kBlock / G;
-  __shared__ Map maps[W][G * V];
-  const uint32_t at = first + blockIdx.x;
-  const int64_t chunk = at / (uint32_t)a.tiles;
-  const Lane<G, XD> l((int)(at % (uint32_t)a.tiles), a.cols);
+template <int G, int XD, int GD, bool Back, bool Free>
+__global__ __launch_bounds__(kBlock) void scan_stretches(const Scan a, unsigned first) {
+  constexpr int V = Width<XD, Back>::value, N = Lanes<G>::value, W = kBlock / N;
+  __shared__ Map maps[W][N * V];
+  const Block block(a, first);
+  const int64_t chunk = block.chunk;
+  const Lane<G, V> l(block.tile, a.cols);
   Map m[V];
-  stretch_of<G, XD, GD, Back, V>(a, l, begin_of<G>(a, chunk, l.w), begin_of<G>(a, chunk, l.w + 1), m);
+  const int64_t nominal = chunk * a.chunk_rows + l.w * a.sub;
+  stretch_of<G, XD, GD, Back, Free, V>(a, l, begin_of<G>(a, nominal), begin_of<G>(a, nominal + a.sub), m);
 #pragma unroll
   for (int q = 0; q < V; ++q) maps[l.w][l.at * V + q] = m[q];
   const int forgets = __syncthreads_or(m[0].a < 0.f);
-  if (l.on)
 #pragma unroll
-    for (int q = 0; q < V; ++q)
-      if (q == 0 || l.both) a.stretch[(chunk * W + l.w) * a.cols + l.c + q] = make_float2(m[q].a, m[q].s);
-  if (l.w == 0 && l.on) {
+  for (int q = 0; q < V; ++q)
+    if (q < l.valid) a.stretch[(chunk * W + l.w) * a.cols + l.c + q] = make_float2(m[q].a, m[q].s);
+  if (l.w == 0) {
 #pragma unroll
     for (int q = 0; q < V; ++q) {
       Map all = {1.f, 0.f};
       for (int w = 0; w < W; ++w) all = after(all, maps[Back ? W - 1 - w : w][l.at * V + q]);
-      if (q == 0 || l.both) a.chunk[chunk * a.cols + l.c + q] = make_float2(all.a, all.s);
+      if (q < l.valid) a.chunk[chunk * a.cols + l.c + q] = make_float2(all.a, all.s);
     }
   }
-  if (threadIdx.x == 0 && at % (uint32_t)a.tiles == 0) a.forgets[chunk] = forgets;
+  if (threadIdx.x == 0 && block.tile == 0) a.forgets[chunk] = forgets;
 }
 
 // The state in front of (behind) a walker's rows: from all chunks since the last one that forgets, then the chunk's walkers.
-template <int G, int XD, int GD, bool Back, bool One, int V>
-__device__ __forceinline__ void state_before(const Scan& a, const Lane<G, XD>& l, int64_t chunk, int lo, int hi, float (&h)[V]) {
-  constexpr int W = kBlock / G;
-  __shared__ Map maps[2][W][G * V];
+template <int G, int XD, int GD, bool Back, bool Free, int V>
+__device__ __forceinline__ void state_before(const Scan& a, const Lane<G, V>& l, int64_t chunk, int lo, int hi, float (&h)[V]) {
+  constexpr int N = Lanes<G>::value, W = kBlock / N;
+  __shared__ Map maps[2][W][N * V];
   __shared__ int nearest;
 #pragma unroll
   for (int q = 0; q < V; ++q) h[q] = 0.f;
-  if constexpr (One) {
-    if (a.whole) return;
-    Map m[V];
-    stretch_of<G, XD, GD, Back, V>(a, l, lo, hi, m);
+  if (a.whole) return;
+  bool goes_on = lo < hi && (Back ? hi < (int)a.rows : lo > 0);
+  if (goes_on) {
+    const int edge = Back ? hi : lo;
+    goes_on = a.seq ? id_of(a, edge) >= 0 && id_of(a, edge) == id_of(a, edge - 1) : edge % a.length != 0;
+  }
+  if (!__syncthreads_or(goes_on)) return;
+  Map m[V];
+  if (a.one) {
+    stretch_of<G, XD, GD, Back, Free, V>(a, l, lo, hi, m);
 #pragma unroll
     for (int q = 0; q < V; ++q) maps[0][l.w][l.at * V + q] = m[q];
     __syncthreads();
   } else {
+    float2 own[V];
+#pragma unroll
+    for (int q = 0; q < V; ++q) own[q] = a.stretch[(chunk * W + l.w) * a.cols + l.c + min(q, l.valid - 1)];
     // chunks between the nearest that forgets (it too) and this one; counted from here on, backwards or forwards
     const int64_t before = Back ? a.chunks - 1 - chunk : chunk;
     int64_t many = before;
@@ -368,7 +410,6 @@ __device__ __forceinline__ void state_before(const Scan& a, const Lane<G, XD>& l
     }
     // farthest first, a share a walker
     const int64_t share = (many + W - 1) / W, from = min(many, l.w * share), to = min(many, from + share);
-    Map m[V];
 #pragma unroll
     for (int q = 0; q < V; ++q) m[q] = {1.f, 0.f};
 #pragma unroll 4
@@ -376,15 +417,14 @@ __device__ __forceinline__ void state_before(const Scan& a, const Lane<G, XD>& l
       const int64_t c = Back ? chunk + many - i : chunk - many + i;
 #pragma unroll
       for (int q = 0; q < V; ++q) {
-        const float2 x = a.chunk[c * a.cols + l.c + (l.both ? q : 0)];
+        const float2 x = a.chunk[c * a.cols + l.c + min(q, l.valid - 1)];
         m[q] = after(m[q], {x.x, x.y});
       }
     }
 #pragma unroll
     for (int q = 0; q < V; ++q) {
       maps[1][l.w][l.at * V + q] = m[q];
-      const float2 x = a.stretch[(chunk * W + l.w) * a.cols + l.c + (l.both ? q : 0)];
-      maps[0][l.w][l.at * V + q] = {x.x, x.y};
+      maps[0][l.w][l.at * V + q] = {own[q].x, own[q].y};
     }
     __syncthreads();
     for (int w = 0; w < W; ++w)
@@ -404,141 +444,229 @@ __device__ __forceinline__ void state_before(const Scan& a, const Lane<G, XD>& l
 
 // ---- the rows
 
-// Row i of a tile, or a row of the walker's own for rows that are not there (read and not used).
-__device__ __forceinline__ int64_t row_at(const Bits& b, int i, int r0, int lo) { return b.there >> i & 1 ? r0 + i : lo; }
+// The tile's rows of a matrix, p the first and a lane's channels `off` bytes in; where a row is not there a row of the walker's own,
+// `own` rows on (read and not used).  (A walker of a whole wave has p in scalar registers, and a load is one instruction.)
+template <int D, int V> __device__ __forceinline__ void load_tile(const char* p, int64_t stride, bool all, uint32_t there, int own, uint32_t off,
+                                                                  int valid, dmt::Raw<D, V> (&x)[kTile]) {
+  if (all) {
+#pragma unroll
+    for (int i = 0; i < kTile; ++i) x[i] = dmt::load_raw<D, V>(p + i * stride + off, valid);
+  } else {
+    const char* instead = p + own * stride;
+#pragma unroll
+    for (int i = 0; i < kTile; ++i) x[i] = dmt::load_raw<D, V>((there >> i & 1 ? p + i * stride : instead) + off, valid);
+  }
+}
+// Whether every walker of the wave says so.
+template <int G> __device__ __forceinline__ bool every(bool x) {
+  if constexpr (G == 64) return x;
+  else return __ballot(!x) == 0;
+}
+// A stride of the loop's turn: its multiples are made there, not held for all rows of every matrix over the loop.
+__device__ __forceinline__ int64_t here(int64_t stride) {
+  asm volatile("" : "+s"(stride));
+  return stride;
+}
+// Bits of the tile's rows in [lo, hi).
+__device__ __forceinline__ uint32_t own_bits(int r0, int lo, int hi) {
+  uint32_t b = kAll;
+  if (r0 < lo) b &= kAll << (lo - r0);
+  if (r0 + kTile > hi) b &= kAll >> (r0 + kTile - hi);
+  return b;
+}
 
-template <int G, int XD, bool One> __global__ __launch_bounds__(kBlock) void scan_fwd(const Scan a, unsigned first) {
-  constexpr int V = Width<XD>::value, EB = dmt::EltBytes<XD>::value;
-  const uint32_t at = first + blockIdx.x;
-  const int64_t chunk = a.chunks - 1 - at / (uint32_t)a.tiles;    // what was read last comes first
-  const Lane<G, XD> l((int)(at % (uint32_t)a.tiles), a.cols);
-  const int lo = begin_of<G>(a, chunk, l.w), hi = begin_of<G>(a, chunk, l.w + 1);
+template <int G, int XD, bool Free> __global__ __launch_bounds__(kBlock) void scan_fwd(const Scan a, unsigned first) {
+  constexpr int V = Width<XD, false>::value, EB = dmt::EltBytes<XD>::value;
+  const Block block(a, first);
+  const int64_t chunk = a.chunks - 1 - block.chunk;               // what was read last comes first
+  const Lane<G, V> l(block.tile, a.cols);
+  const int64_t nominal = chunk * a.chunk_rows + l.w * a.sub;
+  const int lo = begin_of<G>(a, nominal), hi = begin_of<G>(a, nominal + a.sub);
+  const int64_t gate_bytes = a.gate_stride * EB, value_bytes = a.value_stride * EB, h_bytes = a.h_stride * EB;
+  const uint32_t off = (uint32_t)l.c * EB;
+  int r0 = lo & ~(kTile - 1);
+  Bits b = bits_of<G>(a, ids_of(a, r0, lo, hi), r0, lo, hi);
   float h[V];
-  state_before<G, XD, XD, false, One, V>(a, l, chunk, lo, hi, h);
-  const char *gate = a.gate + (int64_t)l.c * EB, *value = a.value + (int64_t)l.c * EB;
-  char* out = a.h + (int64_t)l.c * EB;
-  for (int r0 = lo & ~(kTile - 1); r0 < hi && lo < hi; r0 += kTile) {
-    const Bits b = at % (uint32_t)a.tiles == 0 ? bits_of<G, true>(a, r0, lo, hi) : bits_of<G>(a, r0, lo, hi);
-    if (!l.on) continue;
-    Word<XD, V> g[kTile], v[kTile];
-#pragma unroll
-    for (int i = 0; i < kTile; ++i) {
-      const int64_t r = row_at(b, i, r0, lo);
-      g[i] = load_word<XD, V>(gate + r * a.gate_stride * EB, l.both);
-      v[i] = load_word<XD, V>(value + r * a.value_stride * EB, l.both);
+  state_before<G, XD, XD, false, Free, V>(a, l, chunk, lo, hi, h);
+  if (lo >= hi) return;
+  if (a.seq && a.first_bad && block.tile == 0) report_bad(a, lo, hi, l.at, Lanes<G>::value);
+  for (Bits next; r0 < hi; r0 += kTile, b = next) {
+    const Ids ahead = ids_of(a, r0 + kTile, lo, hi);
+    const uint32_t own = own_bits(r0, lo, hi);
+    if (every<G>(b.there == 0)) {
+      const float zero[V] = {};
+      for (int i = 0; i < kTile; ++i)
+        if (own >> i & 1) dmt::store_elems<XD, V>(a.h + (r0 + i) * h_bytes + off, l.valid, zero);
+      next = bits_of<G>(a, ahead, r0 + kTile, lo, hi);
+      continue;
     }
-    if (a.kept && r0 >= lo)
+    const int64_t gs = here(gate_bytes), vs = here(value_bytes), hs = here(h_bytes);
+    const bool all = every<G>(b.there == kAll);
+    dmt::Raw<XD, V> g[kTile], v[kTile];
+    float start[V];                                       // what the tile's first sequence starts from
+    const int i0 = __builtin_ctz(b.first | 1u << kTile);
+    load_tile<XD, V>(a.gate + r0 * gs, gs, all, b.there, max(lo - r0, 0), off, l.valid, g);
+    load_tile<XD, V>(a.value + r0 * vs, vs, all, b.there, max(lo - r0, 0), off, l.valid, v);
+    load_state<V>(b.first ? a.initial : nullptr, b.id_at(i0), a.cols, l.c, l.valid, start);
+    next = bits_of<G>(a, ahead, r0 + kTile, lo, hi);
+    if (a.kept && r0 >= lo) store_state<V>(a.kept, r0 / kTile, a.cols, l.c, l.valid, h);
+    const auto step = [&](const dmt::Raw<XD, V>& gi, const dmt::Raw<XD, V>& vi) {
+      float s[V], u[V];
+      dmt::unpack<XD, V>(gi, s);
+      dmt::unpack<XD, V>(vi, u);
 #pragma unroll
-      for (int q = 0; q < V; ++q)
-        if (q == 0 || l.both) a.kept[(int64_t)(r0 / kTile) * a.cols + l.c + q] = h[q];
-#pragma unroll
-    for (int i = 0; i < kTile; ++i) {
-      const int r = r0 + i;
-      if (r < lo || r >= hi) continue;
-      float y[V] = {};
-      if (b.there >> i & 1) {
-        if (b.first >> i & 1) {
-          const float* from = a.initial ? a.initial + (int64_t)sequence_of(a, r) * a.cols + l.c : nullptr;
-#pragma unroll
-          for (int q = 0; q < V; ++q) h[q] = from && (q == 0 || l.both) ? from[q] : 0.f;
-        }
-        float x[V], u[V];
-        unpack_word<XD, V>(g[i], x);
-        unpack_word<XD, V>(v[i], u);
-#pragma unroll
-        for (int q = 0; q < V; ++q) {
-          float f, rest;
-          sigmoids(x[q], f, rest);
-          y[q] = h[q] = fmaf(f, h[q], a.free ? u[q] : rest * u[q]);
-        }
-        if ((b.last >> i & 1) && a.final) {
-          float* to = a.final + (int64_t)sequence_of(a, r) * a.cols + l.c;
-#pragma unroll
-          for (int q = 0; q < V; ++q)
-            if (q == 0 || l.both) to[q] = h[q];
-        }
+      for (int q = 0; q < V; ++q) {
+        float f, rest;
+        sigmoids(s[q], f, rest);
+        h[q] = fmaf(f, h[q], Free ? u[q] : rest * u[q]);
+        asm volatile("" : "+v"(h[q]));                    // rounded to float32 before it is to 16 bits, whichever way the tile takes
       }
-      store_word<XD, V>(out + (int64_t)r * a.h_stride * EB, y, l.both);
+    };
+    const auto row = [&](int i) { step(g[i], v[i]); };
+    char* to = a.h + r0 * hs;
+    const uint32_t ends = a.final ? b.last : 0u;
+    if (all && every<G>(b.first == 0 && ends == 0)) {
+#pragma unroll
+      for (int i = 0; i < kTile; ++i) {
+        row(i);
+        dmt::store_elems<XD, V>(to + i * hs + off, l.valid, h);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kTile; ++i) {
+        if (!(own >> i & 1)) continue;
+        float out[V] = {};
+        if (b.there >> i & 1) {
+          if (b.first >> i & 1) {
+            if (i != i0) load_state<V>(a.initial, b.id_at(i), a.cols, l.c, l.valid, start);
+#pragma unroll
+            for (int q = 0; q < V; ++q) h[q] = start[q];
+          }
+          row(i);
+#pragma unroll
+          for (int q = 0; q < V; ++q) out[q] = h[q];
+          if (ends >> i & 1) store_state<V>(a.final, b.id_at(i), a.cols, l.c, l.valid, h);
+        }
+        dmt::store_elems<XD, V>(to + i * hs + off, l.valid, out);
+      }
     }
   }
 }
 
-template <int G, int XD, int GD, bool One> __global__ __launch_bounds__(kBlock) void scan_bwd(const Scan a, unsigned first) {
-  constexpr int V = Width<XD>::value, EB = dmt::EltBytes<XD>::value, GB = dmt::EltBytes<GD>::value;
-  const uint32_t at = first + blockIdx.x;
-  const int64_t chunk = a.chunks - 1 - at / (uint32_t)a.tiles;
-  const Lane<G, XD> l((int)(at % (uint32_t)a.tiles), a.cols);
-  const int lo = begin_of<G>(a, chunk, l.w), hi = begin_of<G>(a, chunk, l.w + 1);
+template <int G, int XD, int GD, bool Free>
+__global__ __launch_bounds__(kBlock) void scan_bwd(const Scan a, unsigned first) {
+  constexpr int V = Width<XD, true>::value, EB = dmt::EltBytes<XD>::value, GB = dmt::EltBytes<GD>::value;
+  const Block block(a, first);
+  const int64_t chunk = a.chunks - 1 - block.chunk;
+  const Lane<G, V> l(block.tile, a.cols);
+  const int64_t nominal = chunk * a.chunk_rows + l.w * a.sub;
+  const int lo = begin_of<G>(a, nominal), hi = begin_of<G>(a, nominal + a.sub);
+  int r0 = (hi - 1) & ~(kTile - 1);
+  Bits b = bits_of<G>(a, ids_of(a, r0, lo, hi), r0, lo, hi);
   float m[V];
-  state_before<G, XD, GD, true, One, V>(a, l, chunk, lo, hi, m);
-  const char *gate = a.gate + (int64_t)l.c * EB, *value = a.value + (int64_t)l.c * EB, *dh = a.dh + (int64_t)l.c * GB;
-  char *dgate = a.dgate + (int64_t)l.c * GB, *dvalue = a.dvalue + (int64_t)l.c * GB;
-  for (int r0 = (hi - 1) & ~(kTile - 1); r0 + kTile > lo && lo < hi; r0 -= kTile) {
-    const Bits b = bits_of<G>(a, r0, lo, hi);
-    if (!l.on) continue;
-    Word<XD, V> g[kTile], v[kTile];
-    Word<GD, V> d[kTile];
-#pragma unroll
-    for (int i = 0; i < kTile; ++i) {
-      const int64_t r = row_at(b, i, r0, lo);
-      g[i] = load_word<XD, V>(gate + r * a.gate_stride * EB, l.both);
-      v[i] = load_word<XD, V>(value + r * a.value_stride * EB, l.both);
-      d[i] = load_word<GD, V>(dh + r * a.dh_stride * GB, l.both);
+  state_before<G, XD, GD, true, Free, V>(a, l, chunk, lo, hi, m);
+  const int64_t gate_bytes = a.gate_stride * EB, value_bytes = a.value_stride * EB, dh_bytes = a.dh_stride * GB;
+  const int64_t dgate_bytes = a.dgate_stride * GB, dvalue_bytes = a.dvalue_stride * GB;
+  const uint32_t off = (uint32_t)l.c * EB, off_g = (uint32_t)l.c * GB;
+  if (lo >= hi) return;
+  for (Bits next; r0 + kTile > lo; r0 -= kTile, b = next) {
+    const Ids ahead = ids_of(a, r0 - kTile, lo, hi);
+    if (every<G>(b.there == 0)) {
+      const uint32_t own = own_bits(r0, lo, hi);
+      const float zero[V] = {};
+      for (int i = 0; i < kTile; ++i)
+        if (own >> i & 1) {
+          dmt::store_elems<GD, V>(a.dgate + (r0 + i) * dgate_bytes + off_g, l.valid, zero);
+          dmt::store_elems<GD, V>(a.dvalue + (r0 + i) * dvalue_bytes + off_g, l.valid, zero);
+        }
+      next = bits_of<G>(a, ahead, r0 - kTile, lo, hi);
+      continue;
     }
-    float h[V] = {};
-    if (r0 >= lo)
-#pragma unroll
-      for (int q = 0; q < V; ++q) h[q] = a.kept[(int64_t)(r0 / kTile) * a.cols + l.c + (l.both ? q : 0)];
-    // f, 1 - f (free: 1) and (h_{t-1} - value) f (1 - f) of the 16 rows
-    float f[kTile][V], share[kTile][V], slope[kTile][V];
-#pragma unroll
-    for (int i = 0; i < kTile; ++i) {
-      if (b.first >> i & 1) {
-        const float* from = a.initial ? a.initial + (int64_t)sequence_of(a, r0 + i) * a.cols + l.c : nullptr;
-#pragma unroll
-        for (int q = 0; q < V; ++q) h[q] = from && (q == 0 || l.both) ? from[q] : 0.f;
-      }
+    const int64_t gs = here(gate_bytes), vs = here(value_bytes), ds = here(dh_bytes), dgs = here(dgate_bytes), dvs = here(dvalue_bytes);
+    const bool all = every<G>(b.there == kAll);
+    dmt::Raw<XD, V> g[kTile], v[kTile];
+    dmt::Raw<GD, V> d[kTile];
+    // the state before the tile, what its first sequence starts from and the gradient that its last one ends with
+    float h[V], start[V], end[V];
+    const int i0 = __builtin_ctz(b.first | 1u << kTile), i1 = 31 - __builtin_clz(b.last | 1u), id0 = b.id_at(i0), id1 = b.id_at(i1);
+    load_tile<XD, V>(a.gate + r0 * gs, gs, all, b.there, max(lo - r0, 0), off, l.valid, g);
+    load_tile<XD, V>(a.value + r0 * vs, vs, all, b.there, max(lo - r0, 0), off, l.valid, v);
+    load_tile<GD, V>(a.dh + r0 * ds, ds, all, b.there, max(lo - r0, 0), off_g, l.valid, d);
+    load_state<V>(r0 >= lo ? a.kept : nullptr, r0 / kTile, a.cols, l.c, l.valid, h);
+    load_state<V>(b.first ? a.initial : nullptr, id0, a.cols, l.c, l.valid, start);
+    load_state<V>(b.last ? a.dfinal : nullptr, id1, a.cols, l.c, l.valid, end);
+    next = bits_of<G>(a, ahead, r0 - kTile, lo, hi);
+    float prev[kTile][V];                                 // the state before each row, forwards; the gradients from them, backwards
+    const auto there = [&](int i) {
+      __builtin_amdgcn_sched_barrier(0);                  // one row after another, or the rows' f and 1 - f are all held at once
       float x[V], u[V];
-      unpack_word<XD, V>(g[i], x);
-      unpack_word<XD, V>(v[i], u);
+      dmt::unpack<XD, V>(g[i], x);
+      dmt::unpack<XD, V>(v[i], u);
 #pragma unroll
       for (int q = 0; q < V; ++q) {
-        float rest;
-        sigmoids(x[q], f[i][q], rest);
-        slope[i][q] = (a.free ? h[q] : h[q] - u[q]) * f[i][q] * rest;
-        share[i][q] = a.free ? 1.f : rest;
-        h[q] = fmaf(f[i][q], h[q], a.free ? u[q] : rest * u[q]);
+        float f, rest;
+        sigmoids(x[q], f, rest);
+        prev[i][q] = h[q];
+        h[q] = fmaf(f, h[q], Free ? u[q] : rest * u[q]);
       }
-    }
+    };
+    const auto back = [&](int i, float (&dg)[V], float (&dv)[V]) {
+      // f and 1 - f are made again: kept over the tile they take 64 registers, and with them a third of the waves
+      dmt::Raw<XD, V> gi = g[i], vi = v[i];
 #pragma unroll
-    for (int i = kTile - 1; i >= 0; --i) {
-      const int r = r0 + i;
-      if (r < lo || r >= hi) continue;
-      float dg[V] = {}, dv[V] = {};
-      if (b.there >> i & 1) {
-        if (b.last >> i & 1) {
-          const float* from = a.dfinal ? a.dfinal + (int64_t)sequence_of(a, r) * a.cols + l.c : nullptr;
+      for (int q = 0; q < dmt::Raw<XD, V>::kWords; ++q) asm volatile("" : "+v"(gi.w[q]), "+v"(vi.w[q]));
+      float x[V], u[V], y[V];
+      dmt::unpack<XD, V>(gi, x);
+      dmt::unpack<XD, V>(vi, u);
+      dmt::unpack<GD, V>(d[i], y);
 #pragma unroll
-          for (int q = 0; q < V; ++q) m[q] = from && (q == 0 || l.both) ? from[q] : 0.f;
-        }
-        float y[V];
-        unpack_word<GD, V>(d[i], y);
-#pragma unroll
-        for (int q = 0; q < V; ++q) {
-          const float lam = y[q] + m[q];
-          dg[q] = lam * slope[i][q];
-          dv[q] = lam * share[i][q];
-          m[q] = f[i][q] * lam;
-        }
-        if ((b.first >> i & 1) && a.dinitial) {
-          float* to = a.dinitial + (int64_t)sequence_of(a, r) * a.cols + l.c;
-#pragma unroll
-          for (int q = 0; q < V; ++q)
-            if (q == 0 || l.both) to[q] = m[q];
-        }
+      for (int q = 0; q < V; ++q) {
+        float f, rest;
+        sigmoids(x[q], f, rest);
+        const float lam = y[q] + m[q], shut = lam * rest;
+        dv[q] = Free ? lam : shut;
+        dg[q] = (Free ? prev[i][q] : prev[i][q] - u[q]) * f * shut;
+        m[q] = f * lam;
       }
-      store_word<GD, V>(dgate + (int64_t)r * a.dgate_stride * GB, dg, l.both);
-      store_word<GD, V>(dvalue + (int64_t)r * a.dvalue_stride * GB, dv, l.both);
+    };
+    char *to_g = a.dgate + r0 * dgs, *to_v = a.dvalue + r0 * dvs;
+    if (all && every<G>((b.first | b.last) == 0)) {
+#pragma unroll
+      for (int i = 0; i < kTile; ++i) there(i);
+#pragma unroll
+      for (int i = kTile - 1; i >= 0; --i) {
+        float dg[V], dv[V];
+        back(i, dg, dv);
+        dmt::store_elems<GD, V>(to_g + i * dgs + off_g, l.valid, dg);
+        dmt::store_elems<GD, V>(to_v + i * dvs + off_g, l.valid, dv);
+      }
+    } else {
+      const uint32_t own = own_bits(r0, lo, hi);
+#pragma unroll
+      for (int i = 0; i < kTile; ++i) {
+        if (b.first >> i & 1) {
+          if (i != i0) load_state<V>(a.initial, b.id_at(i), a.cols, l.c, l.valid, start);
+#pragma unroll
+          for (int q = 0; q < V; ++q) h[q] = start[q];
+        }
+        there(i);                                         // (of no sequence: the next first row forgets it)
+      }
+#pragma unroll
+      for (int i = kTile - 1; i >= 0; --i) {
+        if (!(own >> i & 1)) continue;
+        float dg[V] = {}, dv[V] = {};
+        if (b.there >> i & 1) {
+          if (b.last >> i & 1) {
+            if (i != i1) load_state<V>(a.dfinal, b.id_at(i), a.cols, l.c, l.valid, end);
+#pragma unroll
+            for (int q = 0; q < V; ++q) m[q] = end[q];
+          }
+          back(i, dg, dv);
+          if ((b.first >> i & 1) && a.dinitial) store_state<V>(a.dinitial, b.id_at(i), a.cols, l.c, l.valid, m);
+        }
+        dmt::store_elems<GD, V>(to_g + i * dgs + off_g, l.valid, dg);
+        dmt::store_elems<GD, V>(to_v + i * dvs + off_g, l.valid, dv);
+      }
     }
   }
 }
@@ -615,30 +743,28 @@ __global__ __launch_bounds__(256) void sequence_rows(const int64_t* offsets, int
 
 constexpr int64_t kMost = 1ll << 30;          // rows and sequences: a tile past the last row is still a 32-bit row
 
-// Waves that fill the chip with enough rows requested at once.
-constexpr int64_t kWaves = 2048;
+// Waves that fill the chip with enough rows requested at once; stretches are as long as leaves so many, since a longer one is more
+// often whole sequences, and then the first launch has nothing to read.  131072 x 256 bfloat16 in 4096 ragged sequences: stretches of 32
+// rows 21 + 48 us, of 64 20 + 64.  102400 x 201 float32 in 2048 padded ones, backward: of 64 5 + 111 us, of 32 23 + 101, of 16 32 + 101; forward
+// (16 bytes a lane): of 64 6 + 65, of 32 16 + 64.
+constexpr int64_t waves_for(int elem_bytes) { return elem_bytes == 4 ? 1536 : 4096; }
 
-Cut cut_of(int64_t rows, int64_t cols, int v, bool dense, int64_t sequences) {
+// v: channels of a lane.
+Cut cut_of(int64_t rows, int64_t cols, int elem_bytes, int v, bool dense, int64_t sequences) {
   Cut c = {};
   const int64_t lanes = (cols + v - 1) / v;
-  c.group = lanes <= 16 ? 16 : lanes <= 32 ? 32 : 64;
+  c.group = lanes <= 8 ? 8 : lanes <= 16 ? 16 : lanes <= 32 ? 32 : 64;
   c.tiles = (int)((lanes + c.group - 1) / c.group);
+  c.narrow = cols < v;
   const int64_t walkers = kBlock / c.group;
   auto waves = [&](int64_t sub) { return (rows + sub - 1) / sub * c.tiles * c.group / 64; };
-  if (dense && rows > 0) {
-    const int64_t length = rows / sequences, many = std::max<int64_t>(1, 32 / length);
-    if (waves(length * many) >= kWaves) {
-      c.sub = length * many, c.chunk = c.sub * walkers, c.whole = c.one = true;
-      c.chunks = (rows + c.chunk - 1) / c.chunk;
-      return c;
-    }
-  }
-  c.sub = 64;
-  while (c.sub > 16 && waves(c.sub) < kWaves) c.sub /= 2;
-  if (rows <= walkers * 64) c.sub = std::max<int64_t>(16, (rows + walkers * 16 - 1) / (walkers * 16) * 16);
+  c.sub = kSub;
+  while (c.sub > 2 * kTile && waves(c.sub) < waves_for(elem_bytes)) c.sub /= 2;
+  if (rows <= walkers * kSub) c.sub = std::max<int64_t>(kTile, (rows + walkers * kTile - 1) / (walkers * kTile) * kTile);
   c.chunk = c.sub * walkers;
   c.chunks = std::max<int64_t>(1, (rows + c.chunk - 1) / c.chunk);
-  c.one = c.chunks == 1;
+  c.whole = dense && rows > 0 && rows / sequences <= c.sub;
+  c.one = c.chunks == 1 || c.whole;
   return c;
 }
 
@@ -670,7 +796,7 @@ dmt_status place(Scan& a, const Cut& c, void* workspace, size_t workspace_bytes)
   const size_t need = scratch_bytes(c, a.cols);
   if (need > 0 && !dmt_is_at(workspace, 256)) return DMT_EINVAL;
   if (workspace_bytes < need) return DMT_ENOMEM;
-  a.tiles = c.tiles, a.sub = c.sub, a.chunk_rows = c.chunk, a.chunks = c.chunks, a.whole = c.whole;
+  a.tiles = c.tiles, a.sub = c.sub, a.chunk_rows = c.chunk, a.chunks = c.chunks, a.whole = c.whole, a.one = c.one;
   a.stretch = (float2*)workspace;
   a.chunk = (float2*)((char*)workspace + stretch_bytes(c, a.cols));
   a.forgets = (int*)((char*)a.chunk + chunk_bytes(c, a.cols));
@@ -682,25 +808,25 @@ template <typename Kernel> void launch(Kernel kernel, const Scan& a, hipStream_t
                [&](unsigned first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, a, first); });
 }
 
-template <int G, int XD> void run_fwd(const Scan& a, const Cut& c, hipStream_t s) {
-  if (c.one) {
+template <int G, int XD> void run_fwd(const Scan& a, bool free, hipStream_t s) {
+  if (free) {
+    if (!a.one) launch(scan_stretches<G, XD, XD, false, true>, a, s);
     launch(scan_fwd<G, XD, true>, a, s);
   } else {
-    launch(scan_stretches<G, XD, XD, false>, a, s);
+    if (!a.one) launch(scan_stretches<G, XD, XD, false, false>, a, s);
     launch(scan_fwd<G, XD, false>, a, s);
   }
 }
-template <int G, int XD, int GD> void run_bwd(const Scan& a, const Cut& c, hipStream_t s) {
-  if (c.one) {
-    launch(scan_bwd<G, XD, GD, true>, a, s);
-  } else {
-    launch(scan_stretches<G, XD, GD, true>, a, s);
-    launch(scan_bwd<G, XD, GD, false>, a, s);
-  }
+template <int G, int XD, int GD> void run_bwd(const Scan& a, bool free, hipStream_t s) {
+  if (!a.one) launch(scan_stretches<G, XD, GD, true, false>, a, s);      // (l does not depend on u)
+  if (free) launch(scan_bwd<G, XD, GD, true>, a, s);
+  else launch(scan_bwd<G, XD, GD, false>, a, s);
 }
-template <typename Run> void by_group(int group, Run run) {
-  if (group == 16) run(Int<16>());
-  else if (group == 32) run(Int<32>());
+template <typename Run> void by_group(const Cut& c, Run run) {
+  if (c.narrow) run(Int<0>());
+  else if (c.group == 8) run(Int<8>());
+  else if (c.group == 16) run(Int<16>());
+  else if (c.group == 32) run(Int<32>());
   else run(Int<64>());
 }
 
@@ -720,7 +846,10 @@ extern "C" dmt_status dmt_sequence_rows(const int64_t* offsets, int64_t sequence
 
 extern "C" size_t dmt_gated_scan_workspace_bytes(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 1 || !fits(rows, cols)) return 0;
-  return std::max(scratch_bytes(cut_of(rows, cols, 1, false, 0), cols), scratch_bytes(cut_of(rows, cols, 2, false, 0), cols));
+  size_t most = 0;
+  for (const Cut& c : {cut_of(rows, cols, 2, 4, false, 0), cut_of(rows, cols, 4, 4, false, 0), cut_of(rows, cols, 4, 2, false, 0)})
+    most = std::max(most, scratch_bytes(c, cols));
+  return most;
 }
 
 extern "C" size_t dmt_gated_scan_kept_bytes(int64_t rows, int64_t cols) {
@@ -743,15 +872,15 @@ extern "C" dmt_status dmt_gated_scan_fwd(const void* gate, int64_t gate_stride, 
   a.gate = (const char*)gate, a.value = (const char*)value, a.h = (char*)h;
   a.gate_stride = gate_stride, a.value_stride = value_stride, a.h_stride = h_stride, a.rows = rows, a.cols = (int)cols;
   a.seq = sequence_of, a.sequences = (int)sequences, a.length = sequence_of ? 1 : (int)(rows / sequences);
-  a.initial = initial, a.final = final, a.kept = (float*)kept, a.free = form == DMT_SCAN_FREE, a.first_bad = (unsigned long long*)first_bad;
-  const Cut c = cut_of(rows, cols, dtype == DMT_F32 ? 1 : 2, !sequence_of, sequences);
+  a.initial = initial, a.final = final, a.kept = (float*)kept, a.first_bad = (unsigned long long*)first_bad;
+  const Cut c = cut_of(rows, cols, (int)dmt_ebytes(dtype), 4, !sequence_of, sequences);
   const dmt_status room = place(a, c, workspace, workspace_bytes);
   if (room != DMT_OK) return room;
-  by_group(c.group, [&](auto g) {
+  by_group(c, [&](auto g) {
     constexpr int G = decltype(g)::value;
-    if (dtype == DMT_F32) run_fwd<G, DMT_F32>(a, c, (hipStream_t)stream);
-    else if (dtype == DMT_F16) run_fwd<G, DMT_F16>(a, c, (hipStream_t)stream);
-    else run_fwd<G, DMT_BF16>(a, c, (hipStream_t)stream);
+    if (dtype == DMT_F32) run_fwd<G, DMT_F32>(a, form == DMT_SCAN_FREE, (hipStream_t)stream);
+    else if (dtype == DMT_F16) run_fwd<G, DMT_F16>(a, form == DMT_SCAN_FREE, (hipStream_t)stream);
+    else run_fwd<G, DMT_BF16>(a, form == DMT_SCAN_FREE, (hipStream_t)stream);
   });
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }
@@ -777,18 +906,18 @@ extern "C" dmt_status dmt_gated_scan_bwd(const void* gate, int64_t gate_stride, 
   a.gate_stride = gate_stride, a.value_stride = value_stride, a.dh_stride = dh_stride, a.dgate_stride = dgate_stride;
   a.dvalue_stride = dvalue_stride, a.rows = rows, a.cols = (int)cols;
   a.seq = sequence_of, a.sequences = (int)sequences, a.length = sequence_of ? 1 : (int)(rows / sequences);
-  a.initial = initial, a.dfinal = dfinal, a.dinitial = dinitial, a.kept = (float*)kept, a.free = form == DMT_SCAN_FREE;
-  const Cut c = cut_of(rows, cols, dtype == DMT_F32 ? 1 : 2, !sequence_of, sequences);
+  a.initial = initial, a.dfinal = dfinal, a.dinitial = dinitial, a.kept = (float*)kept;
+  const Cut c = cut_of(rows, cols, (int)dmt_ebytes(dtype), dtype == DMT_F32 ? 2 : 4, !sequence_of, sequences);
   const dmt_status room = place(a, c, workspace, workspace_bytes);
   if (room != DMT_OK) return room;
   hipStream_t s = (hipStream_t)stream;
-  by_group(c.group, [&](auto g) {
+  by_group(c, [&](auto g) {
     constexpr int G = decltype(g)::value;
-    if (dtype == DMT_F32) run_bwd<G, DMT_F32, DMT_F32>(a, c, s);
-    else if (dtype == DMT_F16 && grad_dtype == DMT_F16) run_bwd<G, DMT_F16, DMT_F16>(a, c, s);
-    else if (dtype == DMT_F16) run_bwd<G, DMT_F16, DMT_F32>(a, c, s);
-    else if (grad_dtype == DMT_BF16) run_bwd<G, DMT_BF16, DMT_BF16>(a, c, s);
-    else run_bwd<G, DMT_BF16, DMT_F32>(a, c, s);
+    if (dtype == DMT_F32) run_bwd<G, DMT_F32, DMT_F32>(a, form == DMT_SCAN_FREE, s);
+    else if (dtype == DMT_F16 && grad_dtype == DMT_F16) run_bwd<G, DMT_F16, DMT_F16>(a, form == DMT_SCAN_FREE, s);
+    else if (dtype == DMT_F16) run_bwd<G, DMT_F16, DMT_F32>(a, form == DMT_SCAN_FREE, s);
+    else if (grad_dtype == DMT_BF16) run_bwd<G, DMT_BF16, DMT_BF16>(a, form == DMT_SCAN_FREE, s);
+    else run_bwd<G, DMT_BF16, DMT_F32>(a, form == DMT_SCAN_FREE, s);
   });
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }

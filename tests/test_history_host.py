@@ -150,6 +150,6 @@ def test_expert_combine_bwd_refuses(kw, code):
 def test_workspaces_are_host_arithmetic():
     assert dmt.dmt_gated_scan_workspace_bytes(0, 5) == 0 and dmt.dmt_gated_scan_workspace_bytes(-1, 5) == 0
     assert dmt.dmt_gated_scan_workspace_bytes(10 ** 6, 64) > 0 and dmt.dmt_gated_scan_workspace_bytes(LARGE, 1) == 0
-    assert dmt.dmt_gated_scan_kept_bytes(17, 3) == 24 and dmt.dmt_gated_scan_kept_bytes(0, 3) == 0
+    assert dmt.dmt_gated_scan_kept_bytes(17, 3) == 36 and dmt.dmt_gated_scan_kept_bytes(0, 3) == 0
     assert dmt.dmt_expert_sort_workspace_bytes(10, 2, 8) == 0 and dmt.dmt_expert_sort_workspace_bytes(10 ** 6, 2, 8) > 0
     assert dmt.dmt_expert_sort_workspace_bytes(10 ** 6, 2, 1025) == 0
