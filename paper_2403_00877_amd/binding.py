@@ -658,21 +658,22 @@ def dmt_grad_clip(grad_list, max_norm: float, norm: Optional[torch.Tensor], work
 
 # ---------------------------------------------------------------- the history block
 
-def _here(*tensors: Optional[torch.Tensor]) -> None:
-    """The call's stream is the current device's: so are its tensors."""
+def _here(stream, *tensors: Optional[torch.Tensor]):
+    """The stream's handle.  Its device is the current one; so are the tensors'."""
     device = torch.cuda.current_device()
     for t in tensors:
-        assert t is None or (t.is_cuda and t.get_device() == device), (t.device, device)
+        assert t is None or t.get_device() == device, (t.device, device)
+    return _stream(stream) if stream is not None or _raw_stream is None else _raw_stream(device)
 
 
 def dmt_sequence_rows(offsets: torch.Tensor, sequence_of: torch.Tensor, first_bad: Optional[torch.Tensor] = None,
                       stream=None) -> None:
     """sequence_of[r] = b where offsets[b] <= r < offsets[b + 1], else -1; offsets int64, one more than there are sequences."""
-    _here(offsets, sequence_of, first_bad)
+    on = _here(stream, offsets, sequence_of, first_bad)
     n, rows = offsets.numel(), sequence_of.numel()
     _check("dmt_sequence_rows", _lib.dmt_sequence_rows(
         _vec(offsets, n, torch.int64), n - 1, rows, _vec(sequence_of, rows, torch.int32), _vec(first_bad, 1, torch.int64),
-        _stream(stream)))
+        on))
 
 
 def dmt_gated_scan_workspace_bytes(rows: int, cols: int) -> int:
@@ -689,13 +690,13 @@ def dmt_gated_scan_fwd(gate: torch.Tensor, value: torch.Tensor, h: torch.Tensor,
                        kept: Optional[torch.Tensor] = None, first_bad: Optional[torch.Tensor] = None, stream=None) -> None:
     """h_t = f h_{t-1} + (1 - f) value_t (form "free": + value_t), f = sigmoid(gate_t), along the rows of each sequence."""
     rows, cols = gate.shape
-    _here(gate, value, h, workspace, sequence_of, initial, final, kept, first_bad)
+    on = _here(stream, gate, value, h, workspace, sequence_of, initial, final, kept, first_bad)
     f32, states = torch.float32, sequences * cols
     _check("dmt_gated_scan_fwd", _lib.dmt_gated_scan_fwd(
         gate.data_ptr(), _rows(gate, rows, cols), value.data_ptr(), _rows(value, rows, cols, gate.dtype), rows, cols,
         DTYPE_CODE[gate.dtype], SCAN_FORM_CODE[form], _vec(sequence_of, rows, torch.int32), sequences,
         _vec(initial, states, f32), h.data_ptr(), _rows(h, rows, cols, gate.dtype), _vec(final, states, f32),
-        *_scratch(kept), _vec(first_bad, 1, torch.int64), *_scratch(workspace), _stream(stream)))
+        *_scratch(kept), _vec(first_bad, 1, torch.int64), *_scratch(workspace), on))
 
 
 def dmt_gated_scan_bwd(gate: torch.Tensor, value: torch.Tensor, dh: torch.Tensor, dgate: torch.Tensor,
@@ -705,14 +706,14 @@ def dmt_gated_scan_bwd(gate: torch.Tensor, value: torch.Tensor, dh: torch.Tensor
                        dinitial: Optional[torch.Tensor] = None, stream=None) -> None:
     """Gradients of gate, value and initial from those of h and final; kept as the forward left it."""
     rows, cols = gate.shape
-    _here(gate, value, dh, dgate, dvalue, kept, workspace, sequence_of, initial, dfinal, dinitial)
+    on = _here(stream, gate, value, dh, dgate, dvalue, kept, workspace, sequence_of, initial, dfinal, dinitial)
     f32, states = torch.float32, sequences * cols
     _check("dmt_gated_scan_bwd", _lib.dmt_gated_scan_bwd(
         gate.data_ptr(), _rows(gate, rows, cols), value.data_ptr(), _rows(value, rows, cols, gate.dtype), rows, cols,
         DTYPE_CODE[gate.dtype], SCAN_FORM_CODE[form], _vec(sequence_of, rows, torch.int32), sequences,
         _vec(initial, states, f32), *_scratch(kept), dh.data_ptr(), _rows(dh, rows, cols), DTYPE_CODE[dh.dtype],
         _vec(dfinal, states, f32), dgate.data_ptr(), _rows(dgate, rows, cols, dh.dtype), dvalue.data_ptr(),
-        _rows(dvalue, rows, cols, dh.dtype), _vec(dinitial, states, f32), *_scratch(workspace), _stream(stream)))
+        _rows(dvalue, rows, cols, dh.dtype), _vec(dinitial, states, f32), *_scratch(workspace), on))
 
 
 def dmt_gated_scan_step(gate: torch.Tensor, value: torch.Tensor, state: torch.Tensor, new_state: torch.Tensor,
@@ -721,32 +722,32 @@ def dmt_gated_scan_step(gate: torch.Tensor, value: torch.Tensor, state: torch.Te
     """One row more for the sequences whose states (float32 [states][cols]) slots names; new_state may be state itself."""
     rows, cols = gate.shape
     states = state.shape[0]
-    _here(gate, value, state, new_state, h, slots, first_bad)
+    on = _here(stream, gate, value, state, new_state, h, slots, first_bad)
     _check("dmt_gated_scan_step", _lib.dmt_gated_scan_step(
         gate.data_ptr(), _rows(gate, rows, cols), value.data_ptr(), _rows(value, rows, cols, gate.dtype), rows, cols,
         DTYPE_CODE[gate.dtype], SCAN_FORM_CODE[form], _vec(slots, rows, torch.int32),
         _vec(state, states * cols, torch.float32), _vec(new_state, states * cols, torch.float32), states, h.data_ptr(),
-        _rows(h, rows, cols, gate.dtype), _vec(first_bad, 1, torch.int64), _stream(stream)))
+        _rows(h, rows, cols, gate.dtype), _vec(first_bad, 1, torch.int64), on))
 
 
 def dmt_dropout_fwd(x: torch.Tensor, p: float, rng: torch.Tensor, y: torch.Tensor,
                     residual: Optional[torch.Tensor] = None, site: int = 0, stream=None) -> None:
     """y = residual + (x where it stays) / (1 - p); rng int64 [2] (seed, step) on the GPU."""
     rows, cols = x.shape
-    _here(x, rng, y, residual)
+    on = _here(stream, x, rng, y, residual)
     res, res_stride = (None, 0) if residual is None else (residual.data_ptr(), _rows(residual, rows, cols, x.dtype))
     _check("dmt_dropout_fwd", _lib.dmt_dropout_fwd(
         x.data_ptr(), rows, cols, _rows(x, rows, cols), DTYPE_CODE[x.dtype], res, res_stride, p, _vec(rng, 2, torch.int64),
-        site, y.data_ptr(), _rows(y, rows, cols, x.dtype), _stream(stream)))
+        site, y.data_ptr(), _rows(y, rows, cols, x.dtype), on))
 
 
 def dmt_dropout_bwd(dy: torch.Tensor, p: float, rng: torch.Tensor, dx: torch.Tensor, site: int = 0, stream=None) -> None:
     """dx = (dy where the element stayed) / (1 - p), for the same rng and site as the forward."""
     rows, cols = dy.shape
-    _here(dy, rng, dx)
+    on = _here(stream, dy, rng, dx)
     _check("dmt_dropout_bwd", _lib.dmt_dropout_bwd(
         dy.data_ptr(), rows, cols, _rows(dy, rows, cols), DTYPE_CODE[dy.dtype], p, _vec(rng, 2, torch.int64), site,
-        dx.data_ptr(), _rows(dx, rows, cols, dy.dtype), _stream(stream)))
+        dx.data_ptr(), _rows(dx, rows, cols, dy.dtype), on))
 
 
 def dmt_expert_sort_workspace_bytes(n: int, k: int, num_experts: int) -> int:
@@ -758,12 +759,12 @@ def dmt_expert_sort(experts: torch.Tensor, num_experts: int, slot: torch.Tensor,
                     capacity: int = 0, first_bad: Optional[torch.Tensor] = None, stream=None) -> None:
     """Assignments [n][k] ordered by expert: slot [n][k], source [n * k, or num_experts * capacity], all int32."""
     n, k = experts.shape
-    _here(experts, slot, source, offsets, counts, workspace, first_bad)
+    on = _here(stream, experts, slot, source, offsets, counts, workspace, first_bad)
     i32 = torch.int32
     _check("dmt_expert_sort", _lib.dmt_expert_sort(
         _vec(experts, n * k, i32), n, k, num_experts, capacity, _vec(slot, n * k, i32),
         _vec(source, num_experts * capacity if capacity else n * k, i32), _vec(offsets, num_experts + 1, i32),
-        _vec(counts, num_experts, i32), _vec(first_bad, 1, torch.int64), *_scratch(workspace), _stream(stream)))
+        _vec(counts, num_experts, i32), _vec(first_bad, 1, torch.int64), *_scratch(workspace), on))
 
 
 def _slots(slot: torch.Tensor):
@@ -776,10 +777,10 @@ def dmt_expert_gather(x: torch.Tensor, slot: torch.Tensor, source: torch.Tensor,
     """out[slot[i][j]] = x[i], zeros in rows without an assignment."""
     at, n, k = _slots(slot)
     rows, cols = out.shape
-    _here(x, slot, source, out)
+    on = _here(stream, x, slot, source, out)
     _check("dmt_expert_gather", _lib.dmt_expert_gather(
         x.data_ptr(), n, cols, _rows(x, n, cols, out.dtype), DTYPE_CODE[x.dtype], at, k, _vec(source, rows, torch.int32),
-        rows, out.data_ptr(), _rows(out, rows, cols), _stream(stream)))
+        rows, out.data_ptr(), _rows(out, rows, cols), on))
 
 
 def dmt_expert_combine(z: torch.Tensor, slot: torch.Tensor, weights: Optional[torch.Tensor], y: torch.Tensor,
@@ -787,10 +788,10 @@ def dmt_expert_combine(z: torch.Tensor, slot: torch.Tensor, weights: Optional[to
     """y[i] = the sum over j of weights[i][j] * z[slot[i][j]] (weights None: 1)."""
     at, n, k = _slots(slot)
     rows, cols = z.shape
-    _here(z, slot, weights, y)
+    on = _here(stream, z, slot, weights, y)
     _check("dmt_expert_combine", _lib.dmt_expert_combine(
         z.data_ptr(), rows, cols, _rows(z, rows, cols), DTYPE_CODE[z.dtype], at, n, k, _vec(weights, n * k, torch.float32),
-        y.data_ptr(), _rows(y, n, cols), DTYPE_CODE[y.dtype], _stream(stream)))
+        y.data_ptr(), _rows(y, n, cols), DTYPE_CODE[y.dtype], on))
 
 
 def dmt_expert_combine_bwd(dy: torch.Tensor, z: Optional[torch.Tensor], slot: torch.Tensor,
@@ -800,11 +801,11 @@ def dmt_expert_combine_bwd(dy: torch.Tensor, z: Optional[torch.Tensor], slot: to
     """dz[slot[i][j]] = weights[i][j] * dy[i], zeros elsewhere; dweights[i][j] = dy[i] . z[slot[i][j]]."""
     at, n, k = _slots(slot)
     cols = dy.shape[1]
-    _here(dy, z, slot, source, weights, dz, dweights)
+    on = _here(stream, dy, z, slot, source, weights, dz, dweights)
     rows = z.shape[0] if z is not None else dz.shape[0] if dz is not None else 0
     z_at, z_stride, dtype = (None, cols, dy.dtype) if z is None else (z.data_ptr(), _rows(z, rows, cols), z.dtype)
     dz_at, dz_stride = (None, cols) if dz is None else (dz.data_ptr(), _rows(dz, rows, cols, dy.dtype))
     _check("dmt_expert_combine_bwd", _lib.dmt_expert_combine_bwd(
         dy.data_ptr(), n, cols, _rows(dy, n, cols), DTYPE_CODE[dy.dtype], z_at, rows, z_stride, DTYPE_CODE[dtype], at, k,
         _vec(source, rows, torch.int32), _vec(weights, n * k, torch.float32), dz_at, dz_stride,
-        _vec(dweights, n * k, torch.float32), _stream(stream)))
+        _vec(dweights, n * k, torch.float32), on))

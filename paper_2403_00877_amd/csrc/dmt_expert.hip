@@ -64,10 +64,15 @@ __global__ __launch_bounds__(kSortBlock) void expert_place(const Sort a) {
   int all = 0, before = 0;
   if (e < E) {
     if (a.tiles > 1)
-      for (int t = 0; t < a.tiles; ++t) {
-        const int c = a.part[(int64_t)t * E + e];
-        all += c;
-        before += t < (int)blockIdx.x ? c : 0;
+      for (int t0 = 0; t0 < a.tiles; t0 += 16) {           // 16 rows of counts requested together
+        int c[16];
+#pragma unroll
+        for (int t = 0; t < 16; ++t) c[t] = a.part[(int64_t)min(t0 + t, a.tiles - 1) * E + e];
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+          all += t0 + t < a.tiles ? c[t] : 0;
+          before += t0 + t < (int)blockIdx.x ? c[t] : 0;
+        }
       }
     for (int w = 0; w < kSortWaves; ++w) {
       const int c = place[w * E + e];
@@ -116,8 +121,8 @@ __global__ __launch_bounds__(kSortBlock) void expert_place(const Sort a) {
   // rows without an assignment: behind the last one (of an expert)
   for (int64_t r = (int64_t)blockIdx.x * kSortBlock + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * kSortBlock) {
     if (a.capacity) {
-      const int x = (int)(r / a.capacity);
-      if (r - x * a.capacity >= total[x]) a.source[r] = -1;
+      const uint32_t x = (uint32_t)r / (uint32_t)a.capacity;
+      if ((int)((uint32_t)r - x * (uint32_t)a.capacity) >= total[x]) a.source[r] = -1;
     } else if (r >= (int64_t)sum) {
       a.source[r] = -1;
     }
@@ -125,6 +130,11 @@ __global__ __launch_bounds__(kSortBlock) void expert_place(const Sort a) {
 }
 
 // ------------------------------------------------------------------ rows there and back
+//
+// A group of G lanes has a token, 16 bytes a lane at a time of what is moved (8 elements of what is computed), and takes its assignments
+// four at a time, so that as many rows are under way.  All of it is bound by memory: rows are read once, and written once.
+
+constexpr int kAtOnce = 4;
 
 struct Move {
   const char *x, *z;
@@ -133,99 +143,163 @@ struct Move {
   const int32_t *slot, *source;
   const float* weights;
   float* dweights;
+  unsigned token_blocks;        // blocks that have tokens; those behind them clear rows
   int cols, k;
 };
 
-// Pieces of 16 bytes at a time; a group of 64 lanes has a row.
-template <int EB>
-__global__ __launch_bounds__(kBlock) void expert_gather(const Move a, unsigned first) {
-  constexpr int DT = EB == 4 ? DMT_F32 : DMT_F16, E = 16 / EB;
-  const int64_t r = (int64_t)(first + blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
-  if (r >= a.rows) return;
-  const int s = a.source[r];
-  const bool there = s >= 0 && s / a.k < a.n;
-  const char* from = a.x + (there ? (int64_t)(s / a.k) * a.x_stride : 0) * EB;
-  char* to = a.out + r * a.out_stride * EB;
-  for (int c = (threadIdx.x & 63) * E; c < a.cols; c += 64 * E) {
-    const int valid = min(E, a.cols - c);
-    dmt::Raw<DT, E> v = {};
-    if (there) v = dmt::load_raw<DT, E>(from + (int64_t)c * EB, valid);
-    if (valid == E) {
-      const dmt::dmt_u32x4 w = {v.w[0], v.w[1], v.w[2], v.w[3]};
-      *(DMT_GLOBAL typename dmt::Piece<EB>::v4*)(to + (int64_t)c * EB) = w;
-    } else {
-      for (int i = 0; i < valid; ++i) {
-        if constexpr (EB == 4) *(DMT_GLOBAL uint32_t*)(to + (int64_t)(c + i) * 4) = v.w[i];
-        else *(DMT_GLOBAL uint16_t*)(to + (int64_t)(c + i) * 2) = (uint16_t)(v.w[i / 2] >> i % 2 * 16);
+// A lane's piece of a row, E elements from c on: the last piece of a row of no whole number of them starts earlier, so that it ends with
+// the row (its first `skip` elements are the piece before's too).  Rows shorter than a piece have `valid` elements.
+template <int E> struct Place {
+  int c, skip, valid;
+  __device__ __forceinline__ Place(int at, int cols) {
+    c = max(0, min(at, cols - E));
+    skip = at - c;
+    valid = min(E, cols);
+  }
+};
+
+// The E elements (16 bytes) of type-less words at p.
+template <int EB> __device__ __forceinline__ void store_raw(char* p, int valid, const dmt::Raw<EB == 4 ? DMT_F32 : DMT_F16, 16 / EB>& v) {
+  constexpr int E = 16 / EB;
+  if (valid >= E) {
+    const dmt::dmt_u32x4 w = {v.w[0], v.w[1], v.w[2], v.w[3]};
+    *(DMT_GLOBAL typename dmt::Piece<EB>::v4*)p = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < E - 1; ++i)
+      if (i < valid) {
+        if constexpr (EB == 4) *(DMT_GLOBAL uint32_t*)(p + i * 4) = v.w[i];
+        else *(DMT_GLOBAL uint16_t*)(p + i * 2) = (uint16_t)(v.w[i / 2] >> i % 2 * 16);
       }
+  }
+}
+
+// Zeros into those of the wave's 64 rows that have no assignment.
+template <int EB> __device__ __forceinline__ void clear_rows(const Move& a, int64_t block) {
+  constexpr int E = 16 / EB;
+  const int lane = threadIdx.x & 63;
+  const int64_t r0 = (block * (kBlock / 64) + (threadIdx.x >> 6)) * 64, r = r0 + lane;
+  uint64_t empty = __ballot(r < a.rows && a.source[min(r, a.rows - 1)] < 0);
+  const dmt::Raw<EB == 4 ? DMT_F32 : DMT_F16, E> zero = {};
+  for (; empty; empty &= empty - 1) {
+    char* to = a.out + (r0 + __builtin_ctzll(empty)) * a.out_stride * EB;
+    for (int c = lane * E; c < a.cols; c += 64 * E) {
+      const Place<E> at(c, a.cols);
+      store_raw<EB>(to + (int64_t)at.c * EB, at.valid, zero);
     }
   }
 }
 
-template <int DT, int OD>
-__global__ __launch_bounds__(kBlock) void expert_combine(const Move a, unsigned first) {
-  constexpr int EB = dmt::EltBytes<DT>::value, OB = dmt::EltBytes<OD>::value, E = 8;
-  const int64_t i = (int64_t)(first + blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
-  if (i >= a.n) return;
-  for (int c = (threadIdx.x & 63) * E; c < a.cols; c += 64 * E) {
-    const int valid = min(E, a.cols - c);
-    float sum[E] = {};
-    for (int j = 0; j < a.k; ++j) {
-      const int64_t s = a.slot[i * a.k + j];
-      if (s < 0 || s >= a.rows) continue;
-      const float w = a.weights ? a.weights[i * a.k + j] : 1.f;
-      float v[E];
-      dmt::load_elems<DT, E>(a.z + (s * a.z_stride + c) * EB, valid, v);
+// Token's slots j0 .. j0 + kAtOnce - 1 (-1: none).
+__device__ __forceinline__ void slots_of(const Move& a, int64_t i, int j0, int (&s)[kAtOnce]) {
 #pragma unroll
-      for (int q = 0; q < E; ++q) sum[q] = fmaf(w, v[q], sum[q]);
+  for (int q = 0; q < kAtOnce; ++q) {
+    const int v = j0 + q < a.k ? a.slot[i * a.k + j0 + q] : -1;
+    s[q] = (int64_t)v < a.rows ? v : -1;
+  }
+}
+__device__ __forceinline__ void weights_of(const Move& a, int64_t i, int j0, float (&w)[kAtOnce]) {
+#pragma unroll
+  for (int q = 0; q < kAtOnce; ++q) w[q] = a.weights && j0 + q < a.k ? a.weights[i * a.k + j0 + q] : 1.f;
+}
+
+template <int EB, int G> __global__ __launch_bounds__(kBlock) void expert_gather(const Move a, unsigned first) {
+  constexpr int DT = EB == 4 ? DMT_F32 : DMT_F16, E = 16 / EB;
+  const unsigned block = first + blockIdx.x;
+  if (block >= a.token_blocks) return clear_rows<EB>(a, block - a.token_blocks);
+  const int64_t i = (int64_t)block * (kBlock / G) + threadIdx.x / G;
+  if (i >= a.n) return;
+  for (int j0 = 0; j0 < a.k; j0 += kAtOnce) {
+    int s[kAtOnce];
+    slots_of(a, i, j0, s);
+    for (int c = (threadIdx.x % G) * E; c < a.cols; c += G * E) {
+      const Place<E> at(c, a.cols);
+      const auto v = dmt::load_raw<DT, E>(a.x + (i * a.x_stride + at.c) * EB, at.valid);
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q)
+        if (s[q] >= 0) store_raw<EB>(a.out + (s[q] * a.out_stride + at.c) * EB, at.valid, v);
     }
-    dmt::store_elems<OD, E>(a.out + (i * a.out_stride + c) * OB, valid, sum);
+  }
+}
+
+template <int DT, int OD, int G> __global__ __launch_bounds__(kBlock) void expert_combine(const Move a, unsigned first) {
+  constexpr int EB = dmt::EltBytes<DT>::value, OB = dmt::EltBytes<OD>::value, E = 8;
+  const int64_t i = (int64_t)(first + blockIdx.x) * (kBlock / G) + threadIdx.x / G;
+  if (i >= a.n) return;
+  int s[kAtOnce];
+  float w[kAtOnce];
+  slots_of(a, i, 0, s);
+  weights_of(a, i, 0, w);
+  for (int c = (threadIdx.x % G) * E; c < a.cols; c += G * E) {
+    const Place<E> at(c, a.cols);
+    float sum[E] = {};
+    for (int j0 = 0; j0 < a.k; j0 += kAtOnce) {
+      if (a.k > kAtOnce) {
+        slots_of(a, i, j0, s);
+        weights_of(a, i, j0, w);
+      }
+      dmt::Raw<DT, E> z[kAtOnce];
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        z[q] = {};
+        if (s[q] >= 0) z[q] = dmt::load_raw<DT, E>(a.z + (s[q] * a.z_stride + at.c) * EB, at.valid);
+      }
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        float v[E];
+        dmt::unpack<DT, E>(z[q], v);
+        const float by = s[q] >= 0 ? w[q] : 0.f;
+#pragma unroll
+        for (int p = 0; p < E; ++p) sum[p] = fmaf(by, v[p], sum[p]);
+      }
+    }
+    dmt::store_elems<OD, E>(a.out + (i * a.out_stride + at.c) * OB, at.valid, sum);
   }
 }
 
 // x is dy here, out dz.
-template <int DT, int GD>
-__global__ __launch_bounds__(kBlock) void expert_combine_bwd(const Move a, unsigned first) {
+template <int DT, int GD, int G> __global__ __launch_bounds__(kBlock) void expert_combine_bwd(const Move a, unsigned first) {
   constexpr int EB = dmt::EltBytes<DT>::value, GB = dmt::EltBytes<GD>::value, E = 8;
-  const int64_t i = (int64_t)(first + blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
+  const unsigned block = first + blockIdx.x;
+  if (block >= a.token_blocks) return clear_rows<GB>(a, block - a.token_blocks);
+  const int64_t i = (int64_t)block * (kBlock / G) + threadIdx.x / G;
   if (i >= a.n) return;
-  const int lane = threadIdx.x & 63;
-  for (int j = 0; j < a.k; ++j) {
-    const int64_t s = a.slot[i * a.k + j];
-    const bool there = s >= 0 && s < a.rows;
-    const float w = a.weights ? a.weights[i * a.k + j] : 1.f;
-    float dot = 0.f;
-    for (int c = lane * E; there && c < a.cols; c += 64 * E) {
-      const int valid = min(E, a.cols - c);
-      float g[E], v[E];
-      dmt::load_elems<GD, E>(a.x + (i * a.x_stride + c) * GB, valid, g);
-      if (a.dweights) {
-        dmt::load_elems<DT, E>(a.z + (s * a.z_stride + c) * EB, valid, v);
+  for (int j0 = 0; j0 < a.k; j0 += kAtOnce) {
+    int s[kAtOnce];
+    float w[kAtOnce], dot[kAtOnce] = {};
+    slots_of(a, i, j0, s);
+    weights_of(a, i, j0, w);
+    for (int c = (threadIdx.x % G) * E; c < a.cols; c += G * E) {
+      const Place<E> at(c, a.cols);
+      float g[E];
+      dmt::load_elems<GD, E>(a.x + (i * a.x_stride + at.c) * GB, at.valid, g);
+      dmt::Raw<DT, E> z[kAtOnce];
 #pragma unroll
-        for (int q = 0; q < E; ++q) dot = fmaf(g[q], v[q], dot);
+      for (int q = 0; q < kAtOnce; ++q) {
+        z[q] = {};
+        if (a.dweights && s[q] >= 0) z[q] = dmt::load_raw<DT, E>(a.z + (s[q] * a.z_stride + at.c) * EB, at.valid);
       }
-      if (a.out) {
 #pragma unroll
-        for (int q = 0; q < E; ++q) g[q] *= w;
-        dmt::store_elems<GD, E>(a.out + (s * a.out_stride + c) * GB, valid, g);
+      for (int q = 0; q < kAtOnce; ++q) {
+        if (s[q] < 0) continue;
+        float v[E], d[E];
+        dmt::unpack<DT, E>(z[q], v);
+#pragma unroll
+        for (int p = 0; p < E; ++p) {
+          dot[q] = p >= at.skip ? fmaf(g[p], v[p], dot[q]) : dot[q];
+          d[p] = w[q] * g[p];
+        }
+        if (a.out) dmt::store_elems<GD, E>(a.out + (s[q] * a.out_stride + at.c) * GB, at.valid, d);
       }
     }
     if (a.dweights) {
-      dot = dmt::group_sum<64>(dot);
-      if (lane == 0) a.dweights[i * a.k + j] = dot;
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        dot[q] = dmt::group_sum<G>(dot[q]);
+        if (threadIdx.x % G == 0 && j0 + q < a.k) a.dweights[i * a.k + j0 + q] = dot[q];
+      }
     }
   }
-}
-
-// Zeros into the rows without an assignment.
-template <int EB>
-__global__ __launch_bounds__(kBlock) void expert_clear(const Move a, unsigned first) {
-  constexpr int DT = EB == 4 ? DMT_F32 : DMT_F16, E = 16 / EB;
-  const int64_t r = (int64_t)(first + blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
-  if (r >= a.rows || a.source[r] >= 0) return;
-  const float zero[E] = {};
-  for (int c = (threadIdx.x & 63) * E; c < a.cols; c += 64 * E)
-    dmt::store_elems<DT, E>(a.out + (r * a.out_stride + c) * EB, min(E, a.cols - c), zero);
 }
 
 template <int V> struct Int { static constexpr int value = V; };
@@ -278,10 +352,20 @@ extern "C" dmt_status dmt_expert_sort(const int32_t* experts, int64_t n, int64_t
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }
 
-// Waves, one a row, four to a block.
-template <typename Kernel> static void by_rows(Kernel kernel, const Move& a, int64_t rows, hipStream_t s) {
-  dmt_launches((rows + kBlock / 64 - 1) / (kBlock / 64), kBlock,
-               [&](unsigned first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, a, first); });
+// Groups of lanes that a row of `cols` elements, E a lane, is given: of 4, 16, 32 or 64.
+template <typename Go> static void by_group(int64_t cols, int64_t E, Go go) {
+  const int64_t lanes = (cols + E - 1) / E;
+  if (lanes <= 4) go(Int<4>());
+  else if (lanes <= 16) go(Int<16>());
+  else if (lanes <= 32) go(Int<32>());
+  else go(Int<64>());
+}
+
+// Blocks for the tokens, a group of G lanes each, and then, where rows are cleared, for 64 rows a wave.
+template <typename Kernel> static void by_tokens(Kernel kernel, Move& a, int G, int64_t clear, hipStream_t s) {
+  const int64_t tokens = (a.n + kBlock / G - 1) / (kBlock / G), all = tokens + (clear + kBlock - 1) / kBlock;
+  a.token_blocks = (unsigned)tokens;
+  dmt_launches(all, kBlock, [&](unsigned first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, a, first); });
 }
 
 extern "C" dmt_status dmt_expert_gather(const void* x, int64_t n, int64_t cols, int64_t x_stride, int32_t dtype,
@@ -296,8 +380,11 @@ extern "C" dmt_status dmt_expert_gather(const void* x, int64_t n, int64_t cols, 
   Move a = {};
   a.x = (const char*)x, a.out = (char*)out, a.x_stride = x_stride, a.out_stride = out_stride, a.n = n, a.rows = rows;
   a.slot = slot, a.source = source, a.cols = (int)cols, a.k = (int)k;
-  if (dtype == DMT_F32) by_rows(expert_gather<4>, a, rows, (hipStream_t)stream);
-  else by_rows(expert_gather<2>, a, rows, (hipStream_t)stream);
+  by_group(cols, 16 / e, [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    if (dtype == DMT_F32) by_tokens(expert_gather<4, G>, a, G, rows, (hipStream_t)stream);
+    else by_tokens(expert_gather<2, G>, a, G, rows, (hipStream_t)stream);
+  });
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }
 
@@ -315,7 +402,12 @@ extern "C" dmt_status dmt_expert_combine(const void* z, int64_t rows, int64_t co
   a.z = (const char*)z, a.out = (char*)y, a.z_stride = z_stride, a.out_stride = y_stride, a.n = n, a.rows = rows;
   a.slot = slot, a.weights = weights, a.cols = (int)cols, a.k = (int)k;
   by_type(dtype, [&](auto d) {
-    by_type(y_dtype, [&](auto o) { by_rows(expert_combine<decltype(d)::value, decltype(o)::value>, a, n, (hipStream_t)stream); });
+    by_type(y_dtype, [&](auto o) {
+      by_group(cols, 8, [&](auto g) {
+        constexpr int G = decltype(g)::value;
+        by_tokens(expert_combine<decltype(d)::value, decltype(o)::value, G>, a, G, 0, (hipStream_t)stream);
+      });
+    });
   });
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }
@@ -338,16 +430,14 @@ extern "C" dmt_status dmt_expert_combine_bwd(const void* dy, int64_t n, int64_t 
   a.x = (const char*)dy, a.z = (const char*)z, a.out = (char*)dz, a.x_stride = dy_stride, a.z_stride = z_stride;
   a.out_stride = dz_stride, a.n = n, a.rows = rows, a.slot = slot, a.source = source, a.weights = weights;
   a.dweights = dweights, a.cols = (int)cols, a.k = (int)k;
-  hipStream_t s = (hipStream_t)stream;
-  if (dz && rows > 0) {
-    if (grad_dtype == DMT_F32) by_rows(expert_clear<4>, a, rows, s);
-    else by_rows(expert_clear<2>, a, rows, s);
-  }
-  if (n > 0 && (dz || dweights))
-    by_type(dtype, [&](auto d) {
-      constexpr int D = decltype(d)::value;
-      if (grad_dtype == D) by_rows(expert_combine_bwd<D, D>, a, n, s);
-      else by_rows(expert_combine_bwd<D, DMT_F32>, a, n, s);
+  if (!dz && !dweights) return DMT_OK;
+  by_type(dtype, [&](auto d) {
+    by_group(cols, 8, [&](auto g) {
+      constexpr int D = decltype(d)::value, G = decltype(g)::value;
+      const int64_t clear = dz ? rows : 0;
+      if (grad_dtype == D) by_tokens(expert_combine_bwd<D, D, G>, a, G, clear, (hipStream_t)stream);
+      else by_tokens(expert_combine_bwd<D, DMT_F32, G>, a, G, clear, (hipStream_t)stream);
     });
+  });
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }

@@ -686,22 +686,62 @@ struct Step {
   bool free;
 };
 
-constexpr int kStepBlock = 256;
+constexpr int kStepBlock = 256, kStepRows = 64, kStepBits = 1 << 17;
 
-template <int XD> __global__ __launch_bounds__(kStepBlock) void scan_step(const Step a, unsigned first) {
+// A block has `per` rows (Many) or one.  Whether an earlier row of the call names a row's slot too: one slot is compared with all
+// earlier ones; several set bits (slot mod 2^17), the earlier ones are looked up there, and the few that hit are compared.  (One row a
+// block: 8192 x 64 float16 17 us, 65536 x 64 580.)
+template <int XD, bool Many> __global__ __launch_bounds__(kStepBlock) void scan_step(const Step a, int per, unsigned first) {
   constexpr int EB = dmt::EltBytes<XD>::value, E = 4;
-  const int64_t i = (int64_t)first + blockIdx.x;
-  int64_t slot = i;
+  __shared__ int slots[kStepRows], taken[kStepRows];
+  __shared__ uint32_t bits[Many ? kStepBits / 32 : 1];
+  const int64_t i0 = (int64_t)(first + blockIdx.x) * per;
+  const int m = (int)min((int64_t)per, a.rows - i0), t = threadIdx.x;
   if (a.slots) {
-    slot = a.slots[i];
-    bool taken = false;                                       // by an earlier row
-    for (int64_t j = threadIdx.x; j < i; j += kStepBlock) taken |= a.slots[j] == slot;
-    const bool bad = slot >= 0 && (slot >= a.states || __syncthreads_or(taken));
-    if (bad && threadIdx.x == 0 && a.first_bad) atomicMin(a.first_bad, (unsigned long long)i);
-    if (bad) slot = -1;
+    int raw = -1;
+    if (t < m) {
+      raw = a.slots[i0 + t];
+      slots[t] = raw < a.states ? raw : -1;
+      taken[t] = 0;
+    }
+    if constexpr (Many) {
+      for (int w = t; w < kStepBits / 32; w += kStepBlock) bits[w] = 0;
+      __syncthreads();
+      if (t < m && slots[t] >= 0) atomicOr(&bits[slots[t] % kStepBits / 32], 1u << (slots[t] & 31));
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int64_t j = t * 4; j < i0; j += kStepBlock * 4) {
+      const int many = (int)min((int64_t)4, i0 - j);
+      const auto ids = dmt::load_raw<DMT_F32, 4>((const char*)(a.slots + j), many);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int id = (int)ids.w[q];
+        if (q >= many || id < 0) continue;
+        if constexpr (Many) {
+          if (bits[id % kStepBits / 32] >> (id & 31) & 1)
+            for (int r = 0; r < m; ++r)
+              if (slots[r] == id) taken[r] = 1;
+        } else {
+          if (slots[0] == id) taken[0] = 1;
+        }
+      }
+    }
+    __syncthreads();
+    bool bad = false;
+    if (t < m) {
+      bad = raw >= a.states || taken[t];
+      for (int r = 0; r < t; ++r) bad |= raw >= 0 && slots[r] == raw;
+      if (bad && a.first_bad) atomicMin(a.first_bad, (unsigned long long)(i0 + t));
+    }
+    __syncthreads();
+    if (bad) slots[t] = -1;
+    __syncthreads();
   }
-  for (int c = threadIdx.x * E; c < a.cols; c += kStepBlock * E) {
-    const int valid = min(E, a.cols - c);
+  const int pieces = (a.cols + E - 1) / E;
+  for (int64_t at = t; at < (int64_t)m * pieces; at += kStepBlock) {
+    const int r = (int)((uint64_t)at / (uint32_t)pieces), c = (int)(at - (int64_t)r * pieces) * E, valid = min(E, a.cols - c);
+    const int64_t i = i0 + r, slot = a.slots ? slots[r] : i;
     float y[E] = {};
     if (slot >= 0) {
       float x[E], u[E];
@@ -942,10 +982,13 @@ extern "C" dmt_status dmt_gated_scan_step(const void* gate, int64_t gate_stride,
   a.cols = (int)cols, a.free = form == DMT_SCAN_FREE;
   hipStream_t s = (hipStream_t)stream;
   auto go = [&](auto kernel) {
-    dmt_launches(rows, kStepBlock, [&](unsigned first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kStepBlock), 0, s, a, first); });
+    const int per = slots ? (int)std::min<int64_t>(kStepRows, std::max<int64_t>(1, rows / 512)) : 1;
+    dmt_launches((rows + per - 1) / per, kStepBlock,
+                 [&](unsigned first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kStepBlock), 0, s, a, per, first); });
   };
-  if (dtype == DMT_F32) go(scan_step<DMT_F32>);
-  else if (dtype == DMT_F16) go(scan_step<DMT_F16>);
-  else go(scan_step<DMT_BF16>);
+  const bool many = slots && rows >= 1024;
+  if (dtype == DMT_F32) many ? go(scan_step<DMT_F32, true>) : go(scan_step<DMT_F32, false>);
+  else if (dtype == DMT_F16) many ? go(scan_step<DMT_F16, true>) : go(scan_step<DMT_F16, false>);
+  else many ? go(scan_step<DMT_BF16, true>) : go(scan_step<DMT_BF16, false>);
   return hipGetLastError() == hipSuccess ? DMT_OK : DMT_EHIP;
 }
