@@ -30,14 +30,28 @@ __device__ __forceinline__ void stretch_of(const Sort& a, int64_t& from, int64_t
   to = min(a.m, from + a.stretch);
 }
 
+// Four times 64 assignments from i0 on, a lane's requested together (-1 behind the stretch).
+constexpr int kBatch = 4;
+__device__ __forceinline__ void load_batch(const Sort& a, int64_t i0, int64_t to, int (&e)[kBatch]) {
+#pragma unroll
+  for (int b = 0; b < kBatch; ++b) {
+    const int64_t i = i0 + b * 64 + (threadIdx.x & 63);
+    e[b] = i < to ? a.experts[i] : -1;
+  }
+}
+
 // Counts of the wave's assignments by expert, added to count[E] (LDS, zero).
 __device__ __forceinline__ void count_stretch(const Sort& a, int* count) {
   int64_t from, to;
   stretch_of(a, from, to);
-  for (int64_t i = from + (threadIdx.x & 63); i < to; i += 64) {
-    const int e = a.experts[i];
-    if ((uint32_t)e < (uint32_t)a.E) atomicAdd(&count[e], 1);
-    else if (e >= 0 && a.first_bad) atomicMin(a.first_bad, (unsigned long long)i);
+  for (int64_t i0 = from; i0 < to; i0 += kBatch * 64) {
+    int e[kBatch];
+    load_batch(a, i0, to, e);
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if ((uint32_t)e[b] < (uint32_t)a.E) atomicAdd(&count[e[b]], 1);
+      else if (e[b] >= 0 && a.first_bad) atomicMin(a.first_bad, (unsigned long long)(i0 + b * 64 + (threadIdx.x & 63)));
+    }
   }
 }
 
@@ -95,27 +109,32 @@ __global__ __launch_bounds__(kSortBlock) void expert_place(const Sort a) {
   __syncthreads();
   int64_t from, to;
   stretch_of(a, from, to);
-  for (int64_t i0 = from; i0 < to; i0 += 64) {
-    const int64_t i = i0 + lane;
-    const int x = i < to ? a.experts[i] : -1;
-    const bool named = (uint32_t)x < (uint32_t)E;
-    uint64_t same = __ballot(named);
-    for (int b = 0; b < a.bits; ++b) {
-      const uint64_t set = __ballot((x >> b) & 1);
-      same &= (x >> b) & 1 ? set : ~set;
-    }
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    int base = 0;
-    if (named && rank == 0) base = atomicAdd(&place[wave * E + x], (int)__popcll(same));
-    base = __shfl(base, named ? __ffsll((unsigned long long)same) - 1 : lane);
-    if (i < to) {
-      int64_t row = -1;
-      if (named) {
-        const int64_t r = (int64_t)base + rank;
-        if (!a.capacity || r < a.capacity) row = begin[x] + r;
+  for (int64_t b0 = from; b0 < to; b0 += kBatch * 64) {
+    int e4[kBatch];
+    load_batch(a, b0, to, e4);
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const int64_t i = b0 + b * 64 + lane;
+      const int x = e4[b];
+      const bool named = (uint32_t)x < (uint32_t)E;
+      uint64_t same = __ballot(named);
+      for (int p = 0; p < a.bits; ++p) {
+        const uint64_t set = __ballot((x >> p) & 1);
+        same &= (x >> p) & 1 ? set : ~set;
       }
-      a.slot[i] = (int)row;
-      if (row >= 0) a.source[row] = (int)i;
+      const int rank = __popcll(same & ((1ull << lane) - 1));
+      int base = 0;
+      if (named && rank == 0) base = atomicAdd(&place[wave * E + x], (int)__popcll(same));
+      base = __shfl(base, named ? __ffsll((unsigned long long)same) - 1 : lane);
+      if (i < to) {
+        int64_t row = -1;
+        if (named) {
+          const int64_t r = (int64_t)base + rank;
+          if (!a.capacity || r < a.capacity) row = begin[x] + r;
+        }
+        a.slot[i] = (int)row;
+        if (row >= 0) a.source[row] = (int)i;
+      }
     }
   }
   // rows without an assignment: behind the last one (of an expert)

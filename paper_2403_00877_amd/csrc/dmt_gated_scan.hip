@@ -209,6 +209,39 @@ template <int V> __device__ __forceinline__ void store_state(float* p, int64_t r
   dmt::store_elems<DMT_F32, V>((char*)(p + row * cols) + (uint32_t)c * 4u, valid, x);
 }
 
+// ---- maps of a block's walkers, in the rows' order (Back: against it)
+
+// m: the walker's own -> of all walkers of the wave up to it.
+template <int G, bool Back, int V> __device__ __forceinline__ void join_wave(Map (&m)[V]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = Lanes<G>::value; o < 64; o <<= 1)
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      const Map t = {Back ? __shfl_down(m[q].a, o) : __shfl_up(m[q].a, o), Back ? __shfl_down(m[q].s, o) : __shfl_up(m[q].s, o)};
+      if (Back ? lane + o < 64 : lane >= o) m[q] = after(t, m[q]);
+    }
+}
+// From there: of all walkers of the wave before it.
+template <int G, bool Back, int V> __device__ __forceinline__ void before_in_wave(Map (&m)[V]) {
+  constexpr int N = Lanes<G>::value;
+  const int lane = threadIdx.x & 63;
+  const bool none = Back ? lane + N >= 64 : lane < N;
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    const Map t = {Back ? __shfl_down(m[q].a, N) : __shfl_up(m[q].a, N), Back ? __shfl_down(m[q].s, N) : __shfl_up(m[q].s, N)};
+    m[q] = none ? Map{1.f, 0.f} : t;
+  }
+}
+// The wave's own map, of its last walker, to all.
+template <int G, bool Back, int V, int C> __device__ __forceinline__ void tell_wave(const Map (&m)[V], Map (&waves)[kBlock / 64][C]) {
+  constexpr int N = Lanes<G>::value;
+  const int lane = threadIdx.x & 63;
+  if (Back ? lane < N : lane >= 64 - N)
+#pragma unroll
+    for (int q = 0; q < V; ++q) waves[threadIdx.x >> 6][lane % N * V + q] = m[q];
+}
+
 // ---- what a stretch makes of the state before it
 
 // Rows [from, hi) in their order: A and S.
@@ -343,7 +376,7 @@ __device__ __forceinline__ void stretch_of(const Scan& a, const Lane<G, V>& l, i
 template <int G, int XD, int GD, bool Back, bool Free>
 __global__ __launch_bounds__(kBlock) void scan_stretches(const Scan a, unsigned first) {
   constexpr int V = Width<XD, Back>::value, N = Lanes<G>::value, W = kBlock / N;
-  __shared__ Map maps[W][N * V];
+  __shared__ Map waves[kBlock / 64][N * V];
   const Block block(a, first);
   const int64_t chunk = block.chunk;
   const Lane<G, V> l(block.tile, a.cols);
@@ -351,16 +384,18 @@ __global__ __launch_bounds__(kBlock) void scan_stretches(const Scan a, unsigned 
   const int64_t nominal = chunk * a.chunk_rows + l.w * a.sub;
   stretch_of<G, XD, GD, Back, Free, V>(a, l, begin_of<G>(a, nominal), begin_of<G>(a, nominal + a.sub), m);
 #pragma unroll
-  for (int q = 0; q < V; ++q) maps[l.w][l.at * V + q] = m[q];
-  const int forgets = __syncthreads_or(m[0].a < 0.f);
-#pragma unroll
   for (int q = 0; q < V; ++q)
     if (q < l.valid) a.stretch[(chunk * W + l.w) * a.cols + l.c + q] = make_float2(m[q].a, m[q].s);
+  const bool mine = m[0].a < 0.f;
+  join_wave<G, Back, V>(m);
+  tell_wave<G, Back, V>(m, waves);
+  const int forgets = __syncthreads_or(mine);
   if (l.w == 0) {
 #pragma unroll
     for (int q = 0; q < V; ++q) {
       Map all = {1.f, 0.f};
-      for (int w = 0; w < W; ++w) all = after(all, maps[Back ? W - 1 - w : w][l.at * V + q]);
+#pragma unroll
+      for (int w = 0; w < kBlock / 64; ++w) all = after(all, waves[Back ? kBlock / 64 - 1 - w : w][l.at * V + q]);
       if (q < l.valid) a.chunk[chunk * a.cols + l.c + q] = make_float2(all.a, all.s);
     }
   }
@@ -370,8 +405,8 @@ __global__ __launch_bounds__(kBlock) void scan_stretches(const Scan a, unsigned 
 // The state in front of (behind) a walker's rows: from all chunks since the last one that forgets, then the chunk's walkers.
 template <int G, int XD, int GD, bool Back, bool Free, int V>
 __device__ __forceinline__ void state_before(const Scan& a, const Lane<G, V>& l, int64_t chunk, int lo, int hi, float (&h)[V]) {
-  constexpr int N = Lanes<G>::value, W = kBlock / N;
-  __shared__ Map maps[2][W][N * V];
+  constexpr int N = Lanes<G>::value, W = kBlock / N, Waves = kBlock / 64;
+  __shared__ Map waves[2][Waves][N * V];
   __shared__ int nearest;
 #pragma unroll
   for (int q = 0; q < V; ++q) h[q] = 0.f;
@@ -385,9 +420,6 @@ __device__ __forceinline__ void state_before(const Scan& a, const Lane<G, V>& l,
   Map m[V];
   if (a.one) {
     stretch_of<G, XD, GD, Back, Free, V>(a, l, lo, hi, m);
-#pragma unroll
-    for (int q = 0; q < V; ++q) maps[0][l.w][l.at * V + q] = m[q];
-    __syncthreads();
   } else {
     float2 own[V];
 #pragma unroll
@@ -421,24 +453,26 @@ __device__ __forceinline__ void state_before(const Scan& a, const Lane<G, V>& l,
         m[q] = after(m[q], {x.x, x.y});
       }
     }
+    join_wave<G, false, V>(m);
+    tell_wave<G, false, V>(m, waves[1]);
 #pragma unroll
-    for (int q = 0; q < V; ++q) {
-      maps[1][l.w][l.at * V + q] = m[q];
-      maps[0][l.w][l.at * V + q] = {own[q].x, own[q].y};
-    }
-    __syncthreads();
-    for (int w = 0; w < W; ++w)
-#pragma unroll
-      for (int q = 0; q < V; ++q) h[q] = applied(maps[1][w][l.at * V + q], h[q]);
+    for (int q = 0; q < V; ++q) m[q] = {own[q].x, own[q].y};
   }
-  if constexpr (Back) {
-    for (int w = W - 1; w > l.w; --w)
+  join_wave<G, Back, V>(m);
+  tell_wave<G, Back, V>(m, waves[0]);
+  before_in_wave<G, Back, V>(m);
+  __syncthreads();
+  const int wave = uniform<64>(threadIdx.x >> 6);
 #pragma unroll
-      for (int q = 0; q < V; ++q) h[q] = applied(maps[0][w][l.at * V + q], h[q]);
-  } else {
-    for (int w = 0; w < l.w; ++w)
-#pragma unroll
-      for (int q = 0; q < V; ++q) h[q] = applied(maps[0][w][l.at * V + q], h[q]);
+  for (int q = 0; q < V; ++q) {
+    if (!a.one)
+      for (int w = 0; w < Waves; ++w) h[q] = applied(waves[1][w][l.at * V + q], h[q]);
+    if constexpr (Back) {
+      for (int w = Waves - 1; w > wave; --w) h[q] = applied(waves[0][w][l.at * V + q], h[q]);
+    } else {
+      for (int w = 0; w < wave; ++w) h[q] = applied(waves[0][w][l.at * V + q], h[q]);
+    }
+    h[q] = applied(m[q], h[q]);
   }
 }
 
