@@ -1016,7 +1016,9 @@ extern "C" dmt_status dmt_gated_scan_step(const void* gate, int64_t gate_stride,
   a.cols = (int)cols, a.free = form == DMT_SCAN_FREE;
   hipStream_t s = (hipStream_t)stream;
   auto go = [&](auto kernel) {
-    const int per = slots ? (int)std::min<int64_t>(kStepRows, std::max<int64_t>(1, rows / 512)) : 1;
+    // without slots as many rows as give every thread four pieces
+    const int64_t want = slots ? rows / 512 : 4 * kStepBlock * 4 / cols;
+    const int per = (int)std::min<int64_t>(kStepRows, std::max<int64_t>(1, slots ? want : std::min(want, rows / 512)));
     dmt_launches((rows + per - 1) / per, kStepBlock,
                  [&](unsigned first, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(kStepBlock), 0, s, a, per, first); });
   };

@@ -468,3 +468,169 @@ def test_rows_and_tokens_past_32_bits(dmt):
         assert torch.equal(far, small.flip(0))
         dmt.dmt_expert_combine(far, slot, None, near)
         assert torch.equal(near, small)
+
+
+# ------------------------------------------------------------------ nothing, streams, graphs
+
+def test_calls_of_nothing(dmt):
+    f32 = lambda *shape: torch.full(shape, 7.0, device="cuda")
+    i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device="cuda")
+    x, state, rng = f32(0, 24), f32(3, 24), torch.zeros(2, dtype=torch.int64, device="cuda")
+    for seq, n in ((i32(0), 3), (None, 0), (None, 3)):
+        final, dinitial = f32(n, 24), f32(n, 24)
+        dmt.dmt_gated_scan_fwd(x, x, x, None, sequence_of=seq, sequences=n, final=final)
+        dmt.dmt_gated_scan_bwd(x, x, x, x, x, None, None, sequence_of=seq, sequences=n, dinitial=dinitial)
+        assert bool((final == 7).all()) and bool((dinitial == 7).all())       # sequences without rows are left as they were
+    dmt.dmt_gated_scan_step(x, x, state, state, x, i32(0))
+    dmt.dmt_dropout_fwd(x, 0.5, rng, x)
+    dmt.dmt_dropout_bwd(x, 0.5, rng, x)
+    slot, source = i32(0, 2), torch.full((12,), 9, dtype=torch.int32, device="cuda")
+    offsets, counts = i32(5) + 9, i32(4) + 9
+    dmt.dmt_expert_sort(i32(0, 2), 4, slot, source, offsets, counts, None, capacity=3)
+    assert source.tolist() == [-1] * 12 and offsets.tolist() == [0, 3, 6, 9, 12] and counts.tolist() == [0] * 4
+    out = f32(12, 24)
+    dmt.dmt_expert_gather(x, slot, source, out)                               # no tokens: every row is empty
+    assert bool((out == 0).all())
+    out = f32(12, 24)
+    dmt.dmt_expert_combine(out, slot, None, x)
+    dmt.dmt_expert_combine_bwd(x, None, slot, source, None, out)
+    assert bool((out == 0).all())
+    y, none = f32(5, 24), i32(0)
+    dmt.dmt_expert_combine(x, torch.full((5, 2), -1, dtype=torch.int32, device="cuda"), None, y)      # no rows: sums of nothing
+    assert bool((y == 0).all()) and none.numel() == 0
+    # only rows of no sequence
+    h, final = f32(20, 24), f32(2, 24)
+    ws = bytes_buf(dmt.dmt_gated_scan_workspace_bytes(20, 24))
+    dmt.dmt_gated_scan_fwd(f32(20, 24) / 0, f32(20, 24) / 0, h, ws, sequence_of=i32(20) - 1, sequences=2, final=final)
+    assert bool((h == 0).all()) and bool((final == 7).all())
+
+
+def _block(dmt, seed):
+    """State of a small chain of all operators; run(s) goes through it once."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    n, C, E, k, cap = 700, 72, 6, 2, 200
+    rnd = lambda *shape: torch.randn(*shape, generator=g, device="cuda")
+    f32 = lambda *shape: torch.zeros(*shape, device="cuda")
+    i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device="cuda")
+    s = dict(n=n, C=C, E=E, cap=cap, gate=rnd(n, C) * 2, value=rnd(n, C), off=torch.tensor([0, 5, 5, 300, 690], device="cuda"),
+             seq=i32(n), h=f32(n, C), final=f32(4, C), r=f32(n, C), rng=torch.tensor([seed, 0], device="cuda"),
+             experts=torch.randint(-1, E, (n, k), generator=g, device="cuda", dtype=torch.int32), slot=i32(n, k), source=i32(E * cap),
+             offsets=i32(E + 1), counts=i32(E), rows=f32(E * cap, C), w=rnd(n, k), y=f32(n, C), dz=f32(E * cap, C), dw=f32(n, k),
+             dx=f32(n, C), dh=f32(n, C), dg=f32(n, C), dv=f32(n, C), state=rnd(50, C), slots=torch.randperm(50, generator=g, device="cuda")[:20]
+             .to(torch.int32), new=f32(50, C), hs=f32(20, C),
+             kept=bytes_buf(dmt.dmt_gated_scan_kept_bytes(n, C)), ws=bytes_buf(max(dmt.dmt_gated_scan_workspace_bytes(n, C),
+                                                                                  dmt.dmt_expert_sort_workspace_bytes(n, k, E))))
+    return s
+
+
+def _run_block(dmt, s, stream=None):
+    kw = dict(stream=stream)
+    dmt.dmt_sequence_rows(s["off"], s["seq"], **kw)
+    dmt.dmt_gated_scan_fwd(s["gate"], s["value"], s["h"], s["ws"], sequence_of=s["seq"], sequences=4, final=s["final"], kept=s["kept"], **kw)
+    dmt.dmt_dropout_fwd(s["h"], 0.3, s["rng"], s["r"], residual=s["value"], site=2, **kw)
+    dmt.dmt_expert_sort(s["experts"], s["E"], s["slot"], s["source"], s["offsets"], s["counts"], s["ws"], s["cap"], **kw)
+    dmt.dmt_expert_gather(s["r"], s["slot"], s["source"], s["rows"], **kw)
+    dmt.dmt_expert_combine(s["rows"], s["slot"], s["w"], s["y"], **kw)
+    dmt.dmt_expert_combine_bwd(s["y"], s["rows"], s["slot"], s["source"], s["w"], s["dz"], s["dw"], **kw)
+    dmt.dmt_expert_combine(s["dz"], s["slot"], None, s["dx"], **kw)
+    dmt.dmt_dropout_bwd(s["dx"], 0.3, s["rng"], s["dh"], site=2, **kw)
+    dmt.dmt_gated_scan_bwd(s["gate"], s["value"], s["dh"], s["dg"], s["dv"], s["kept"], s["ws"], sequence_of=s["seq"], sequences=4, **kw)
+    dmt.dmt_gated_scan_step(s["gate"][:20], s["value"][:20], s["state"], s["new"], s["hs"], s["slots"], **kw)
+
+
+OUT = ["seq", "h", "final", "r", "slot", "source", "offsets", "counts", "rows", "y", "dz", "dw", "dx", "dh", "dg", "dv", "new", "hs"]
+
+
+def _cleared(s):
+    for o in OUT:
+        s[o].fill_(-5)
+
+
+def test_another_stream_and_graphs_that_share_a_workspace_give_the_same(dmt):
+    a, b = _block(dmt, 1), _block(dmt, 2)
+    b["ws"] = a["ws"]                                       # ordered by the caller: one after another
+    eager = []
+    for s in (a, b):
+        _cleared(s)                                         # (rows that no call writes stay so)
+        _run_block(dmt, s)
+        eager.append({o: s[o].clone() for o in OUT})
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    _cleared(a)
+    side.wait_stream(torch.cuda.current_stream())
+    _run_block(dmt, a, side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a[o], eager[0][o]) for o in OUT)
+    graphs = []
+    for s in (a, b):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            _run_block(dmt, s)
+        graphs.append(graph)
+    for turn in range(4):
+        for i, s in ((0, a), (1, b)) if turn % 2 == 0 else ((1, b), (0, a)):
+            _cleared(s)
+            if turn == 3:                                   # the replay reads what the tensors hold now: other masks
+                s["rng"][1] = 5
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            if turn < 3:
+                assert all(torch.equal(s[o], eager[i][o]) for o in OUT), (turn, i)
+            else:
+                by_graph = {o: s[o].clone() for o in OUT}
+                assert not torch.equal(by_graph["r"], eager[i]["r"]) and torch.equal(by_graph["h"], eager[i]["h"])
+                _cleared(s)
+                _run_block(dmt, s)
+                assert all(torch.equal(s[o], by_graph[o]) for o in OUT)
+
+
+def test_step_of_many_rows_with_the_same_slot(dmt):
+    rng = np.random.default_rng(8)
+    rows, cols, states = 6000, 8, 300_000
+    slots = rng.permutation(states)[:rows].astype(np.int32)
+    slots[3000:3100] = slots[:100]                           # far behind
+    slots[5001] = slots[5000]                                # in one block
+    slots[4096 * 1 + 7] = slots[2] + 131072 if slots[2] + 131072 < states else -1      # the same bit, another slot
+    slots[200:220] = -4
+    first = {}
+    want_bad = []
+    for i, v in enumerate(slots):
+        if v >= 0 and first.setdefault(int(v), i) != i:
+            want_bad.append(i)
+    gate = torch.full((rows, cols), -100.0, device="cuda")   # shut: the state becomes the value
+    value = torch.arange(rows, device="cuda", dtype=torch.float32)[:, None].expand(rows, cols).contiguous()
+    state, h, bad = torch.full((states, cols), -7.0, device="cuda"), torch.empty(rows, cols, device="cuda"), no_bad()
+    dmt.dmt_gated_scan_step(gate, value, state, state, h, torch.from_numpy(slots).cuda(), first_bad=bad)
+    assert int(bad.cpu()) == want_bad[0]
+    want = np.full(states, -7.0)
+    for v, i in first.items():
+        want[v] = i
+    assert np.allclose(state[:, 0].cpu().numpy(), want, rtol=0, atol=1e-30)
+    refused = np.isin(np.arange(rows), want_bad) | (slots < 0)
+    assert np.array_equal(h[:, 3].cpu().numpy() == 0, refused | (np.arange(rows) == 0))
+
+
+def test_tensors_that_are_refused(dmt):
+    x = torch.ones(4, 8, device="cuda")
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    ws, rng = bytes_buf(1 << 16), torch.zeros(2, dtype=torch.int64, device="cuda")
+    calls = [lambda: dmt.dmt_gated_scan_fwd(x, x.cpu(), x, ws), lambda: dmt.dmt_gated_scan_fwd(x, x[:, :7], x, ws),
+             lambda: dmt.dmt_gated_scan_fwd(x, x.half(), x, ws), lambda: dmt.dmt_gated_scan_fwd(x, x, x, ws.cpu()),
+             lambda: dmt.dmt_gated_scan_fwd(x, x, x, ws, sequence_of=ids.long(), sequences=1),
+             lambda: dmt.dmt_gated_scan_fwd(x, x, x, ws, initial=x), lambda: dmt.dmt_gated_scan_fwd(x, x.t().contiguous().t(), x, ws),
+             lambda: dmt.dmt_gated_scan_step(x, x, x, x[:3], x, ids), lambda: dmt.dmt_gated_scan_step(x, x, x.half(), x, x, ids),
+             lambda: dmt.dmt_dropout_fwd(x, 0.5, rng.cpu(), x), lambda: dmt.dmt_dropout_fwd(x, 0.5, rng[:1], x),
+             lambda: dmt.dmt_dropout_fwd(x, 0.5, rng, x, residual=x.half()), lambda: dmt.dmt_dropout_bwd(x, 0.5, rng, x.half()),
+             lambda: dmt.dmt_expert_gather(x, ids[:, None], ids[:3], x), lambda: dmt.dmt_expert_gather(x.half(), ids[:, None], ids, x),
+             lambda: dmt.dmt_expert_combine(x, ids[:, None].long(), None, x),
+             lambda: dmt.dmt_expert_combine(x, ids[:, None], x, x),
+             lambda: dmt.dmt_expert_sort(ids[:, None], 3, ids[:, None], ids[:3], None, None, ws)]
+    for i, c in enumerate(calls):
+        with pytest.raises(AssertionError):
+            c()
+            raise ValueError("call %d was taken" % i)
+    for c in (lambda: dmt.dmt_gated_scan_fwd(x, x, x, ws, form="other"),):
+        with pytest.raises(KeyError):
+            c()
