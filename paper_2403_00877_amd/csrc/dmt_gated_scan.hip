@@ -21,7 +21,9 @@
 
 namespace {
 
-constexpr int kBlock = 512, kTile = 8, kRun = 16, kSub = 64;
+// Threads of a block; rows of a tile, of a turn of the first launch; the longest stretch's; channels of a lane.  (Two channels a lane: backward of 102400 x 201
+// float32 111 us for 88, one: 120.  Eight of bfloat16: forward of 131072 x 512 no faster, of 131072 x 256 ragged 59 for 50: twice the registers.)
+constexpr int kBlock = 512, kTile = 8, kRun = 16, kSub = 64, V = 4;
 constexpr uint32_t kAll = (1u << kTile) - 1;
 
 // How rows are cut.
@@ -148,9 +150,6 @@ __device__ __forceinline__ void report_bad(const Scan& a, int lo, int hi, int at
     }
 }
 
-// Channels of a lane: four forwards; 8 bytes of the rows' type backwards, where more registers are held.
-template <int XD, bool Back> struct Width { static constexpr int value = Back ? 8 / dmt::EltBytes<XD>::value : 4; };
-
 // f = sigmoid(x) and 1 - f from e = exp(-x): f = 1 / (1 + e), 1 - f = e f.  The product x log2 e is rounded, so e is off by up to 1.25 |x|
 // units of 2^-24 and two more; f and 1 - f then by f (1 - f) times that, at most 0.35 units, and by a few units of their own.  Where e
 // passes the largest float f is 0 and 1 - f is 1 (the minimum takes the number, not inf * 0); a NaN stays in f.
@@ -186,7 +185,7 @@ __device__ __forceinline__ Map after(Map l, Map r) {         // l, then r
 __device__ __forceinline__ float applied(Map m, float h) { return m.a < 0.f ? m.s : fmaf(m.a, h, m.s); }
 
 // What a lane knows about its channels.
-template <int G, int V> struct Lane {
+template <int G> struct Lane {
   static constexpr int N = Lanes<G>::value;
   int w, at, c, valid;     // walker, lane of it, first channel, how many there are
   __device__ __forceinline__ Lane(int tile, int cols) {
@@ -200,19 +199,19 @@ template <int G, int V> struct Lane {
 };
 
 // A lane's channels of a row of a float32 [rows][cols] (null: zeros); and back.
-template <int V> __device__ __forceinline__ void load_state(const float* p, int64_t row, int cols, int c, int valid, float (&x)[V]) {
+__device__ __forceinline__ void load_state(const float* p, int64_t row, int cols, int c, int valid, float (&x)[V]) {
 #pragma unroll
   for (int q = 0; q < V; ++q) x[q] = 0.f;
   if (p) dmt::load_elems<DMT_F32, V>((const char*)(p + row * cols) + (uint32_t)c * 4u, valid, x);
 }
-template <int V> __device__ __forceinline__ void store_state(float* p, int64_t row, int cols, int c, int valid, const float (&x)[V]) {
+__device__ __forceinline__ void store_state(float* p, int64_t row, int cols, int c, int valid, const float (&x)[V]) {
   dmt::store_elems<DMT_F32, V>((char*)(p + row * cols) + (uint32_t)c * 4u, valid, x);
 }
 
 // ---- maps of a block's walkers, in the rows' order (Back: against it)
 
 // m: the walker's own -> of all walkers of the wave up to it.
-template <int G, bool Back, int V> __device__ __forceinline__ void join_wave(Map (&m)[V]) {
+template <int G, bool Back> __device__ __forceinline__ void join_wave(Map (&m)[V]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = Lanes<G>::value; o < 64; o <<= 1)
@@ -223,7 +222,7 @@ template <int G, bool Back, int V> __device__ __forceinline__ void join_wave(Map
     }
 }
 // From there: of all walkers of the wave before it.
-template <int G, bool Back, int V> __device__ __forceinline__ void before_in_wave(Map (&m)[V]) {
+template <int G, bool Back> __device__ __forceinline__ void before_in_wave(Map (&m)[V]) {
   constexpr int N = Lanes<G>::value;
   const int lane = threadIdx.x & 63;
   const bool none = Back ? lane + N >= 64 : lane < N;
@@ -234,7 +233,7 @@ template <int G, bool Back, int V> __device__ __forceinline__ void before_in_wav
   }
 }
 // The wave's own map, of its last walker, to all.
-template <int G, bool Back, int V, int C> __device__ __forceinline__ void tell_wave(const Map (&m)[V], Map (&waves)[kBlock / 64][C]) {
+template <int G, bool Back, int C> __device__ __forceinline__ void tell_wave(const Map (&m)[V], Map (&waves)[kBlock / 64][C]) {
   constexpr int N = Lanes<G>::value;
   const int lane = threadIdx.x & 63;
   if (Back ? lane < N : lane >= 64 - N)
@@ -245,7 +244,7 @@ template <int G, bool Back, int V, int C> __device__ __forceinline__ void tell_w
 // ---- what a stretch makes of the state before it
 
 // Rows [from, hi) in their order: A and S.
-template <int XD, bool Free, int V>
+template <int XD, bool Free>
 __device__ __forceinline__ void map_fwd(const Scan& a, int c, int valid, int from, int hi, float (&A)[V], float (&S)[V]) {
   constexpr int EB = dmt::EltBytes<XD>::value;
   const int64_t gs = a.gate_stride * EB, vs = a.value_stride * EB;
@@ -285,7 +284,7 @@ __device__ __forceinline__ void map_fwd(const Scan& a, int c, int valid, int fro
 }
 
 // Rows [lo, to] against their order: m -> A m + S.
-template <int XD, int GD, int V>
+template <int XD, int GD>
 __device__ __forceinline__ void map_bwd(const Scan& a, int c, int valid, int lo, int to, float (&A)[V], float (&S)[V]) {
   constexpr int EB = dmt::EltBytes<XD>::value, GB = dmt::EltBytes<GD>::value;
   const int64_t gs = a.gate_stride * EB, ds = a.dh_stride * GB;
@@ -326,8 +325,8 @@ __device__ __forceinline__ void map_bwd(const Scan& a, int c, int valid, int lo,
 
 // The map of rows [lo, hi) (backwards: against their order).  Only what the next (the previous) row continues is read: nothing
 // where a sequence starts there, else from the last first (to the first last) row on.
-template <int G, int XD, int GD, bool Back, bool Free, int V>
-__device__ __forceinline__ void stretch_of(const Scan& a, const Lane<G, V>& l, int lo, int hi, Map (&m)[V]) {
+template <int G, int XD, int GD, bool Back, bool Free>
+__device__ __forceinline__ void stretch_of(const Scan& a, const Lane<G>& l, int lo, int hi, Map (&m)[V]) {
   constexpr int N = Lanes<G>::value;
   float A[V], S[V];
 #pragma unroll
@@ -362,9 +361,9 @@ __device__ __forceinline__ void stretch_of(const Scan& a, const Lane<G, V>& l, i
       if (forgets) at = begin;
     }
     if (on) {
-      if (forgets) load_state<V>(Back ? a.dfinal : a.initial, sequence_of(a, inner), a.cols, l.c, l.valid, S);
-      if constexpr (Back) map_bwd<XD, GD, V>(a, l.c, l.valid, lo, at, A, S);
-      else map_fwd<XD, Free, V>(a, l.c, l.valid, at, hi, A, S);
+      if (forgets) load_state(Back ? a.dfinal : a.initial, sequence_of(a, inner), a.cols, l.c, l.valid, S);
+      if constexpr (Back) map_bwd<XD, GD>(a, l.c, l.valid, lo, at, A, S);
+      else map_fwd<XD, Free>(a, l.c, l.valid, at, hi, A, S);
     } else {
       forgets = true;
     }
@@ -375,20 +374,20 @@ __device__ __forceinline__ void stretch_of(const Scan& a, const Lane<G, V>& l, i
 
 template <int G, int XD, int GD, bool Back, bool Free>
 __global__ __launch_bounds__(kBlock) void scan_stretches(const Scan a, unsigned first) {
-  constexpr int V = Width<XD, Back>::value, N = Lanes<G>::value, W = kBlock / N;
+  constexpr int N = Lanes<G>::value, W = kBlock / N;
   __shared__ Map waves[kBlock / 64][N * V];
   const Block block(a, first);
   const int64_t chunk = block.chunk;
-  const Lane<G, V> l(block.tile, a.cols);
+  const Lane<G> l(block.tile, a.cols);
   Map m[V];
   const int64_t nominal = chunk * a.chunk_rows + l.w * a.sub;
-  stretch_of<G, XD, GD, Back, Free, V>(a, l, begin_of<G>(a, nominal), begin_of<G>(a, nominal + a.sub), m);
+  stretch_of<G, XD, GD, Back, Free>(a, l, begin_of<G>(a, nominal), begin_of<G>(a, nominal + a.sub), m);
 #pragma unroll
   for (int q = 0; q < V; ++q)
     if (q < l.valid) a.stretch[(chunk * W + l.w) * a.cols + l.c + q] = make_float2(m[q].a, m[q].s);
   const bool mine = m[0].a < 0.f;
-  join_wave<G, Back, V>(m);
-  tell_wave<G, Back, V>(m, waves);
+  join_wave<G, Back>(m);
+  tell_wave<G, Back>(m, waves);
   const int forgets = __syncthreads_or(mine);
   if (l.w == 0) {
 #pragma unroll
@@ -403,8 +402,8 @@ __global__ __launch_bounds__(kBlock) void scan_stretches(const Scan a, unsigned 
 }
 
 // The state in front of (behind) a walker's rows: from all chunks since the last one that forgets, then the chunk's walkers.
-template <int G, int XD, int GD, bool Back, bool Free, int V>
-__device__ __forceinline__ void state_before(const Scan& a, const Lane<G, V>& l, int64_t chunk, int lo, int hi, float (&h)[V]) {
+template <int G, int XD, int GD, bool Back, bool Free>
+__device__ __forceinline__ void state_before(const Scan& a, const Lane<G>& l, int64_t chunk, int lo, int hi, float (&h)[V]) {
   constexpr int N = Lanes<G>::value, W = kBlock / N, Waves = kBlock / 64;
   __shared__ Map waves[2][Waves][N * V];
   __shared__ int nearest;
@@ -419,7 +418,7 @@ __device__ __forceinline__ void state_before(const Scan& a, const Lane<G, V>& l,
   if (!__syncthreads_or(goes_on)) return;
   Map m[V];
   if (a.one) {
-    stretch_of<G, XD, GD, Back, Free, V>(a, l, lo, hi, m);
+    stretch_of<G, XD, GD, Back, Free>(a, l, lo, hi, m);
   } else {
     float2 own[V];
 #pragma unroll
@@ -453,14 +452,14 @@ __device__ __forceinline__ void state_before(const Scan& a, const Lane<G, V>& l,
         m[q] = after(m[q], {x.x, x.y});
       }
     }
-    join_wave<G, false, V>(m);
-    tell_wave<G, false, V>(m, waves[1]);
+    join_wave<G, false>(m);
+    tell_wave<G, false>(m, waves[1]);
 #pragma unroll
     for (int q = 0; q < V; ++q) m[q] = {own[q].x, own[q].y};
   }
-  join_wave<G, Back, V>(m);
-  tell_wave<G, Back, V>(m, waves[0]);
-  before_in_wave<G, Back, V>(m);
+  join_wave<G, Back>(m);
+  tell_wave<G, Back>(m, waves[0]);
+  before_in_wave<G, Back>(m);
   __syncthreads();
   const int wave = uniform<64>(threadIdx.x >> 6);
 #pragma unroll
@@ -480,7 +479,7 @@ __device__ __forceinline__ void state_before(const Scan& a, const Lane<G, V>& l,
 
 // The tile's rows of a matrix, p the first and a lane's channels `off` bytes in; where a row is not there a row of the walker's own,
 // `own` rows on (read and not used).  (A walker of a whole wave has p in scalar registers, and a load is one instruction.)
-template <int D, int V> __device__ __forceinline__ void load_tile(const char* p, int64_t stride, bool all, uint32_t there, int own, uint32_t off,
+template <int D> __device__ __forceinline__ void load_tile(const char* p, int64_t stride, bool all, uint32_t there, int own, uint32_t off,
                                                                   int valid, dmt::Raw<D, V> (&x)[kTile]) {
   if (all) {
 #pragma unroll
@@ -510,10 +509,10 @@ __device__ __forceinline__ uint32_t own_bits(int r0, int lo, int hi) {
 }
 
 template <int G, int XD, bool Free> __global__ __launch_bounds__(kBlock) void scan_fwd(const Scan a, unsigned first) {
-  constexpr int V = Width<XD, false>::value, EB = dmt::EltBytes<XD>::value;
+  constexpr int EB = dmt::EltBytes<XD>::value;
   const Block block(a, first);
   const int64_t chunk = a.chunks - 1 - block.chunk;               // what was read last comes first
-  const Lane<G, V> l(block.tile, a.cols);
+  const Lane<G> l(block.tile, a.cols);
   const int64_t nominal = chunk * a.chunk_rows + l.w * a.sub;
   const int lo = begin_of<G>(a, nominal), hi = begin_of<G>(a, nominal + a.sub);
   const int64_t gate_bytes = a.gate_stride * EB, value_bytes = a.value_stride * EB, h_bytes = a.h_stride * EB;
@@ -521,7 +520,7 @@ template <int G, int XD, bool Free> __global__ __launch_bounds__(kBlock) void sc
   int r0 = lo & ~(kTile - 1);
   Bits b = bits_of<G>(a, ids_of(a, r0, lo, hi), r0, lo, hi);
   float h[V];
-  state_before<G, XD, XD, false, Free, V>(a, l, chunk, lo, hi, h);
+  state_before<G, XD, XD, false, Free>(a, l, chunk, lo, hi, h);
   if (lo >= hi) return;
   if (a.seq && a.first_bad && block.tile == 0) report_bad(a, lo, hi, l.at, Lanes<G>::value);
   for (Bits next; r0 < hi; r0 += kTile, b = next) {
@@ -539,11 +538,11 @@ template <int G, int XD, bool Free> __global__ __launch_bounds__(kBlock) void sc
     dmt::Raw<XD, V> g[kTile], v[kTile];
     float start[V];                                       // what the tile's first sequence starts from
     const int i0 = __builtin_ctz(b.first | 1u << kTile);
-    load_tile<XD, V>(a.gate + r0 * gs, gs, all, b.there, max(lo - r0, 0), off, l.valid, g);
-    load_tile<XD, V>(a.value + r0 * vs, vs, all, b.there, max(lo - r0, 0), off, l.valid, v);
-    load_state<V>(b.first ? a.initial : nullptr, b.id_at(i0), a.cols, l.c, l.valid, start);
+    load_tile<XD>(a.gate + r0 * gs, gs, all, b.there, max(lo - r0, 0), off, l.valid, g);
+    load_tile<XD>(a.value + r0 * vs, vs, all, b.there, max(lo - r0, 0), off, l.valid, v);
+    load_state(b.first ? a.initial : nullptr, b.id_at(i0), a.cols, l.c, l.valid, start);
     next = bits_of<G>(a, ahead, r0 + kTile, lo, hi);
-    if (a.kept && r0 >= lo) store_state<V>(a.kept, r0 / kTile, a.cols, l.c, l.valid, h);
+    if (a.kept && r0 >= lo) store_state(a.kept, r0 / kTile, a.cols, l.c, l.valid, h);
     const auto step = [&](const dmt::Raw<XD, V>& gi, const dmt::Raw<XD, V>& vi) {
       float s[V], u[V];
       dmt::unpack<XD, V>(gi, s);
@@ -572,14 +571,14 @@ template <int G, int XD, bool Free> __global__ __launch_bounds__(kBlock) void sc
         float out[V] = {};
         if (b.there >> i & 1) {
           if (b.first >> i & 1) {
-            if (i != i0) load_state<V>(a.initial, b.id_at(i), a.cols, l.c, l.valid, start);
+            if (i != i0) load_state(a.initial, b.id_at(i), a.cols, l.c, l.valid, start);
 #pragma unroll
             for (int q = 0; q < V; ++q) h[q] = start[q];
           }
           row(i);
 #pragma unroll
           for (int q = 0; q < V; ++q) out[q] = h[q];
-          if (ends >> i & 1) store_state<V>(a.final, b.id_at(i), a.cols, l.c, l.valid, h);
+          if (ends >> i & 1) store_state(a.final, b.id_at(i), a.cols, l.c, l.valid, h);
         }
         dmt::store_elems<XD, V>(to + i * hs + off, l.valid, out);
       }
@@ -589,16 +588,16 @@ template <int G, int XD, bool Free> __global__ __launch_bounds__(kBlock) void sc
 
 template <int G, int XD, int GD, bool Free>
 __global__ __launch_bounds__(kBlock) void scan_bwd(const Scan a, unsigned first) {
-  constexpr int V = Width<XD, true>::value, EB = dmt::EltBytes<XD>::value, GB = dmt::EltBytes<GD>::value;
+  constexpr int EB = dmt::EltBytes<XD>::value, GB = dmt::EltBytes<GD>::value;
   const Block block(a, first);
   const int64_t chunk = a.chunks - 1 - block.chunk;
-  const Lane<G, V> l(block.tile, a.cols);
+  const Lane<G> l(block.tile, a.cols);
   const int64_t nominal = chunk * a.chunk_rows + l.w * a.sub;
   const int lo = begin_of<G>(a, nominal), hi = begin_of<G>(a, nominal + a.sub);
   int r0 = (hi - 1) & ~(kTile - 1);
   Bits b = bits_of<G>(a, ids_of(a, r0, lo, hi), r0, lo, hi);
   float m[V];
-  state_before<G, XD, GD, true, Free, V>(a, l, chunk, lo, hi, m);
+  state_before<G, XD, GD, true, Free>(a, l, chunk, lo, hi, m);
   const int64_t gate_bytes = a.gate_stride * EB, value_bytes = a.value_stride * EB, dh_bytes = a.dh_stride * GB;
   const int64_t dgate_bytes = a.dgate_stride * GB, dvalue_bytes = a.dvalue_stride * GB;
   const uint32_t off = (uint32_t)l.c * EB, off_g = (uint32_t)l.c * GB;
@@ -623,12 +622,12 @@ __global__ __launch_bounds__(kBlock) void scan_bwd(const Scan a, unsigned first)
     // the state before the tile, what its first sequence starts from and the gradient that its last one ends with
     float h[V], start[V], end[V];
     const int i0 = __builtin_ctz(b.first | 1u << kTile), i1 = 31 - __builtin_clz(b.last | 1u), id0 = b.id_at(i0), id1 = b.id_at(i1);
-    load_tile<XD, V>(a.gate + r0 * gs, gs, all, b.there, max(lo - r0, 0), off, l.valid, g);
-    load_tile<XD, V>(a.value + r0 * vs, vs, all, b.there, max(lo - r0, 0), off, l.valid, v);
-    load_tile<GD, V>(a.dh + r0 * ds, ds, all, b.there, max(lo - r0, 0), off_g, l.valid, d);
-    load_state<V>(r0 >= lo ? a.kept : nullptr, r0 / kTile, a.cols, l.c, l.valid, h);
-    load_state<V>(b.first ? a.initial : nullptr, id0, a.cols, l.c, l.valid, start);
-    load_state<V>(b.last ? a.dfinal : nullptr, id1, a.cols, l.c, l.valid, end);
+    load_tile<XD>(a.gate + r0 * gs, gs, all, b.there, max(lo - r0, 0), off, l.valid, g);
+    load_tile<XD>(a.value + r0 * vs, vs, all, b.there, max(lo - r0, 0), off, l.valid, v);
+    load_tile<GD>(a.dh + r0 * ds, ds, all, b.there, max(lo - r0, 0), off_g, l.valid, d);
+    load_state(r0 >= lo ? a.kept : nullptr, r0 / kTile, a.cols, l.c, l.valid, h);
+    load_state(b.first ? a.initial : nullptr, id0, a.cols, l.c, l.valid, start);
+    load_state(b.last ? a.dfinal : nullptr, id1, a.cols, l.c, l.valid, end);
     next = bits_of<G>(a, ahead, r0 - kTile, lo, hi);
     float prev[kTile][V];                                 // the state before each row, forwards; the gradients from them, backwards
     const auto there = [&](int i) {
@@ -679,7 +678,7 @@ __global__ __launch_bounds__(kBlock) void scan_bwd(const Scan a, unsigned first)
 #pragma unroll
       for (int i = 0; i < kTile; ++i) {
         if (b.first >> i & 1) {
-          if (i != i0) load_state<V>(a.initial, b.id_at(i), a.cols, l.c, l.valid, start);
+          if (i != i0) load_state(a.initial, b.id_at(i), a.cols, l.c, l.valid, start);
 #pragma unroll
           for (int q = 0; q < V; ++q) h[q] = start[q];
         }
@@ -691,12 +690,12 @@ __global__ __launch_bounds__(kBlock) void scan_bwd(const Scan a, unsigned first)
         float dg[V] = {}, dv[V] = {};
         if (b.there >> i & 1) {
           if (b.last >> i & 1) {
-            if (i != i1) load_state<V>(a.dfinal, b.id_at(i), a.cols, l.c, l.valid, end);
+            if (i != i1) load_state(a.dfinal, b.id_at(i), a.cols, l.c, l.valid, end);
 #pragma unroll
             for (int q = 0; q < V; ++q) m[q] = end[q];
           }
           back(i, dg, dv);
-          if ((b.first >> i & 1) && a.dinitial) store_state<V>(a.dinitial, b.id_at(i), a.cols, l.c, l.valid, m);
+          if ((b.first >> i & 1) && a.dinitial) store_state(a.dinitial, b.id_at(i), a.cols, l.c, l.valid, m);
         }
         dmt::store_elems<GD, V>(to_g + i * dgs + off_g, l.valid, dg);
         dmt::store_elems<GD, V>(to_v + i * dvs + off_g, l.valid, dv);
@@ -819,17 +818,15 @@ constexpr int64_t kMost = 1ll << 30;          // rows and sequences: a tile past
 
 // Waves that fill the chip with enough rows requested at once; stretches are as long as leaves so many, since a longer one is more
 // often whole sequences, and then the first launch has nothing to read.  131072 x 256 bfloat16 in 4096 ragged sequences: stretches of 32
-// rows 21 + 48 us, of 64 20 + 64.  102400 x 201 float32 in 2048 padded ones, backward: of 64 5 + 111 us, of 32 23 + 101, of 16 32 + 101; forward
-// (16 bytes a lane): of 64 6 + 65, of 32 16 + 64.
+// rows 21 + 48 us, of 64 20 + 64.  102400 x 201 float32 in 2048 padded ones (a lane has twice the bytes): of 64 6 + 65, of 32 16 + 64, of 16 26 + 62.
 constexpr int64_t waves_for(int elem_bytes) { return elem_bytes == 4 ? 1536 : 4096; }
 
-// v: channels of a lane.
-Cut cut_of(int64_t rows, int64_t cols, int elem_bytes, int v, bool dense, int64_t sequences) {
+Cut cut_of(int64_t rows, int64_t cols, int elem_bytes, bool dense, int64_t sequences) {
   Cut c = {};
-  const int64_t lanes = (cols + v - 1) / v;
+  const int64_t lanes = (cols + V - 1) / V;
   c.group = lanes <= 8 ? 8 : lanes <= 16 ? 16 : lanes <= 32 ? 32 : 64;
   c.tiles = (int)((lanes + c.group - 1) / c.group);
-  c.narrow = cols < v;
+  c.narrow = cols < V;
   const int64_t walkers = kBlock / c.group;
   auto waves = [&](int64_t sub) { return (rows + sub - 1) / sub * c.tiles * c.group / 64; };
   c.sub = kSub;
@@ -920,10 +917,7 @@ extern "C" dmt_status dmt_sequence_rows(const int64_t* offsets, int64_t sequence
 
 extern "C" size_t dmt_gated_scan_workspace_bytes(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 1 || !fits(rows, cols)) return 0;
-  size_t most = 0;
-  for (const Cut& c : {cut_of(rows, cols, 2, 4, false, 0), cut_of(rows, cols, 4, 4, false, 0), cut_of(rows, cols, 4, 2, false, 0)})
-    most = std::max(most, scratch_bytes(c, cols));
-  return most;
+  return std::max(scratch_bytes(cut_of(rows, cols, 2, false, 0), cols), scratch_bytes(cut_of(rows, cols, 4, false, 0), cols));
 }
 
 extern "C" size_t dmt_gated_scan_kept_bytes(int64_t rows, int64_t cols) {
@@ -947,7 +941,7 @@ extern "C" dmt_status dmt_gated_scan_fwd(const void* gate, int64_t gate_stride, 
   a.gate_stride = gate_stride, a.value_stride = value_stride, a.h_stride = h_stride, a.rows = rows, a.cols = (int)cols;
   a.seq = sequence_of, a.sequences = (int)sequences, a.length = sequence_of ? 1 : (int)(rows / sequences);
   a.initial = initial, a.final = final, a.kept = (float*)kept, a.first_bad = (unsigned long long*)first_bad;
-  const Cut c = cut_of(rows, cols, (int)dmt_ebytes(dtype), 4, !sequence_of, sequences);
+  const Cut c = cut_of(rows, cols, (int)dmt_ebytes(dtype), !sequence_of, sequences);
   const dmt_status room = place(a, c, workspace, workspace_bytes);
   if (room != DMT_OK) return room;
   by_group(c, [&](auto g) {
@@ -981,7 +975,7 @@ extern "C" dmt_status dmt_gated_scan_bwd(const void* gate, int64_t gate_stride, 
   a.dvalue_stride = dvalue_stride, a.rows = rows, a.cols = (int)cols;
   a.seq = sequence_of, a.sequences = (int)sequences, a.length = sequence_of ? 1 : (int)(rows / sequences);
   a.initial = initial, a.dfinal = dfinal, a.dinitial = dinitial, a.kept = (float*)kept;
-  const Cut c = cut_of(rows, cols, (int)dmt_ebytes(dtype), dtype == DMT_F32 ? 2 : 4, !sequence_of, sequences);
+  const Cut c = cut_of(rows, cols, (int)dmt_ebytes(dtype), !sequence_of, sequences);
   const dmt_status room = place(a, c, workspace, workspace_bytes);
   if (room != DMT_OK) return room;
   hipStream_t s = (hipStream_t)stream;
