@@ -4,7 +4,8 @@
 // the backward makes it again and nothing is stored.
 //
 // A thread has eight elements (16 bytes of a 16-bit type); rows start a new counter, so an odd width leaves a part of its last eight
-// unused.
+// unused.  Bound by memory: the generator is some 20 wide products and 60 plain instructions for eight elements.  262144 x 256 bfloat16
+// with the residual 71 us, 5.7 TB/s; 65536 x 1024 without 46, x 1021 in rows of 1026 55; 65536 x 333 float32 38, 4.7 TB/s.
 #include "dmt_internal.h"
 #include "dmt_rows.h"
 

@@ -4,7 +4,8 @@
 // block's; there are at most 64 tiles, so that a block finds the counts before it by adding up to 64 rows of counts itself and no
 // launch of its own scans them.  Inside a tile every wave has a stretch of its own and ranks 64 assignments at a time: the
 // lanes that name the same expert are found with one ballot a bit of the expert's number.  Places depend on the assignments'
-// order alone.  One tile needs one launch.
+// order alone.  One tile needs one launch.  65536 x 2 assignments to 64 experts 4.5 + 8.9 us, 131072 x 8 to 256 7.7 + 25.6, 64 x 2 4.2: chains of
+// latencies, of the counts before a tile (16 rows of them requested together: 17 us for 9) and of four times 64 ranks.
 #include <algorithm>
 
 #include "dmt_internal.h"
@@ -151,7 +152,9 @@ __global__ __launch_bounds__(kSortBlock) void expert_place(const Sort a) {
 // ------------------------------------------------------------------ rows there and back
 //
 // A group of G lanes has a token, 16 bytes a lane at a time of what is moved (8 elements of what is computed), and takes its assignments
-// four at a time, so that as many rows are under way.  All of it is bound by memory: rows are read once, and written once.
+// four at a time, so that as many rows are under way.  All of it is bound by memory: rows are read once, and written once.  65536 tokens of 512
+// bfloat16 to two of 64 experts 46 us, 5.1 TB/s (by rows of the order, a token's row read twice: 67); back from four, 32768 x 1024, 65 us, 5.1 TB/s;
+// gradients of 32768 x 512 in float32 61 + 37 us.
 
 constexpr int kAtOnce = 4;
 

@@ -12,8 +12,9 @@
 // The backward needs h_{t-1}: the forward keeps the state in front of every 8th row in float32, from which a walker goes through
 // its 8 rows again, so neither h nor a rounded h is read.
 //
-// Bound by memory: two sequences of 65536 x 512 bfloat16, forward 81 + 87 us (the rows read twice, 268 MB each time, and 151 MB
-// written), backward 63 + 138 (671 MB in the second launch, 4.9 TB/s); 131072 x 256 bfloat16 in 4096 ragged sequences 21 + 48 us.
+// Bound by memory where sequences are long: two of 65536 x 512 bfloat16, forward 79 + 86 us (the rows are read twice, 268 MB each time,
+// and 168 MB written), backward 64 + 139 (688 MB in the second launch, 4.9 TB/s).  4096 ragged ones, 131072 x 256 bfloat16, 21 + 51 us.  2048 padded
+// ones, 102400 x 201 float32, forward 6 + 63 us, backward 5 + 86.
 #include <algorithm>
 
 #include "dmt_internal.h"
