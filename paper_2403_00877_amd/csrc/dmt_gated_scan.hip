@@ -24,14 +24,14 @@ namespace {
 
 // Threads of a block; rows of a tile, of a turn of the first launch; the longest stretch's; channels of a lane.  (Two channels a lane: backward of 102400 x 201
 // float32 111 us for 88, one: 120.  Eight of bfloat16: forward of 131072 x 512 no faster, of 131072 x 256 ragged 59 for 50: twice the registers.)
-constexpr int kBlock = 512, kTile = 8, kRun = 16, kSub = 64, V = 4;
+constexpr int kBlock = 512, kTile = 8, kRun = 16, kSub = 64, kRoom = 32, V = 4;
 constexpr uint32_t kAll = (1u << kTile) - 1;
 
 // How rows are cut.
 struct Cut {
   int group;           // lanes of a walker: 8, 16, 32 or 64
   int tiles;           // groups' widths of channels
-  int64_t sub;         // rows of a walker nominally, a multiple of kTile unless `whole`
+  int64_t sub;         // rows of a walker nominally
   int64_t chunk;       // rows of a chunk
   int64_t chunks;
   bool whole;          // every walker starts with a sequence's first row: equal ones, none longer than a stretch
@@ -68,15 +68,17 @@ __device__ __forceinline__ int id_of(const Scan& a, int row) {
 }
 __device__ __forceinline__ int sequence_of(const Scan& a, int row) { return a.seq ? id_of(a, row) : row / a.length; }
 
-// Where the rows of the walker whose nominal first row is b begin: where the sequence changes next, if it does within the stretch, else b.
-// So walkers have whole sequences where those are short, and only long ones are cut.
+// Where the rows of the walker whose nominal first row is b begin: where the sequence changes next, if it does within the stretch, else at
+// b's tile, in front of whose first row the state is kept.  So walkers have whole sequences where those are short, and only long ones are cut.
+// (The stretch is looked through up to the next one's tile, so that beginnings ascend.)
 template <int G> __device__ __forceinline__ int begin_of(const Scan& a, int64_t nominal) {
   constexpr int N = Lanes<G>::value, Steps = kSub / N;
   if (nominal >= a.rows) return (int)a.rows;
-  const int b = (int)nominal, end = (int)min((int64_t)a.rows, nominal + a.sub), lane = threadIdx.x & 63;
+  const int64_t past = (nominal + a.sub) & ~(int64_t)(kTile - 1);
+  const int b = (int)nominal, end = (int)min(a.rows, past), lane = threadIdx.x & 63;
   if (!a.seq) {
     const int next = (b + a.length - 1) / a.length * a.length;
-    return next < nominal + a.sub ? next : b;
+    return next < past ? next : b & ~(kTile - 1);
   }
   int here[Steps], before[Steps];
 #pragma unroll
@@ -85,7 +87,7 @@ template <int G> __device__ __forceinline__ int begin_of(const Scan& a, int64_t 
     here[i] = id_of(a, row);
     before[i] = id_of(a, max(row - 1, 0));
   }
-  int found = b;
+  int found = b & ~(kTile - 1);
 #pragma unroll
   for (int i = Steps - 1; i >= 0; --i) {
     const int row = b + i * N + lane % N;
@@ -841,6 +843,10 @@ Cut cut_of(int64_t rows, int64_t cols, int elem_bytes, bool dense, int64_t seque
   } else {
     c.sub = kSub;
     while (c.sub > 2 * kTile && waves(c.sub) < waves_for(elem_bytes)) c.sub /= 2;
+    // rooms of a padded batch begin where stretches of their length do: 2048 of 50 x 201 float32 56 + 74 us for 69 + 92; where that leaves few
+    // waves, and the rows are ragged, it costs (262144 x 16 bfloat16 in 4096 sequences, 512 waves: 91 + 131 for 40 + 52)
+    const int64_t room = !dense && sequences > 0 && rows % sequences == 0 ? rows / sequences : 0;
+    if (room >= kRoom && room <= kSub && waves(room) >= 1024) c.sub = room;
   }
   c.chunk = c.sub * walkers;
   c.chunks = std::max<int64_t>(1, (rows + c.chunk - 1) / c.chunk);
@@ -926,7 +932,17 @@ extern "C" dmt_status dmt_sequence_rows(const int64_t* offsets, int64_t sequence
 
 extern "C" size_t dmt_gated_scan_workspace_bytes(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 1 || !fits(rows, cols)) return 0;
-  return std::max(scratch_bytes(cut_of(rows, cols, 2, false, 0), cols), scratch_bytes(cut_of(rows, cols, 4, false, 0), cols));
+  // of either type, and with the shortest stretch that rooms can bring
+  size_t most = 0;
+  for (int elem_bytes : {2, 4}) {
+    Cut c = cut_of(rows, cols, elem_bytes, false, 0);
+    if (!c.one && c.sub > kRoom) {
+      c.chunk = c.chunk / c.sub * kRoom;
+      c.chunks = (rows + c.chunk - 1) / c.chunk;
+    }
+    most = std::max(most, scratch_bytes(c, cols));
+  }
+  return most;
 }
 
 extern "C" size_t dmt_gated_scan_kept_bytes(int64_t rows, int64_t cols) {

@@ -35,6 +35,10 @@ def sequences_of(rng, kind, rows, sequences):
     if kind == "equal":
         return None
     order = rng.permutation(sequences)
+    if kind == "room":
+        room = rows // sequences
+        there = np.arange(room) < rng.integers(0, room + 1, sequences)[:, None]
+        return np.where(there, order[:, None], -1).reshape(-1).astype(np.int32)
     seq = np.repeat(order, lengths_of(rng, rows, sequences))
     if kind == "holes":                       # rows of no sequence: some stretches, the front, the end; ids past the last
         for _ in range(max(1, rows // 40)):
@@ -134,6 +138,14 @@ def test_gated_scan(dmt, rows, cols, sequences, pad, shift, kind, dtype, gd):
                                                        (105_000, 64, 2_100, "f32"), (68_000, 300, 4_000, "f32")])
 def test_gated_scan_of_many_equal_sequences(dmt, rows, cols, sequences, dtype):
     scan_case(dmt, rows, cols, sequences, 0, 0, dtype, dtype, "equal", False, True)
+
+
+@pytest.mark.parametrize("kind", ["room", "ragged"])
+@pytest.mark.parametrize("room", [32, 33, 37, 50, 63, 64])
+@pytest.mark.parametrize("cols,sequences,dtype", [(300, 60, "bf16"), (70, 90, "f32"), (9, 150, "f16")])
+def test_gated_scan_of_padded_rooms(dmt, room, cols, sequences, dtype, kind):
+    """Rows in as many equal rooms as sequences, and sequences of any length whose mean is a room."""
+    scan_case(dmt, room * sequences, cols, sequences, 0, 0, dtype, dtype, kind, False, True, seed=room)
 
 
 @pytest.mark.parametrize("rows,cols,starts", [(400_000, 64, [0]), (400_000, 64, [0, 131, 399_990]), (300_000, 5, [0, 250_000]),
