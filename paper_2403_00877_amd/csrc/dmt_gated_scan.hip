@@ -12,9 +12,9 @@
 // The backward needs h_{t-1}: the forward keeps the state in front of every 8th row in float32, from which a walker goes through
 // its 8 rows again, so neither h nor a rounded h is read.
 //
-// Bound by memory where sequences are long: two of 65536 x 512 bfloat16, forward 79 + 86 us (the rows are read twice, 268 MB each time,
-// and 168 MB written), backward 64 + 139 (688 MB in the second launch, 4.9 TB/s).  4096 ragged ones, 131072 x 256 bfloat16, 21 + 51 us.  2048 padded
-// ones, 102400 x 201 float32, forward 6 + 63 us, backward 5 + 86.
+// Bound by memory where sequences are long: two of 65536 x 512 bfloat16, forward 80 + 87 us (the rows are read twice, 268 MB each time,
+// and 168 MB written), backward 64 + 139 (688 MB in the second launch, 4.9 TB/s).  4096 ragged ones, 131072 x 256 bfloat16, 21 + 50 us.  2048 padded
+// ones, 102400 x 201 float32, forward 6 + 50 us, backward 5 + 68.  4096 of 64 x 256 bfloat16 whole, one launch each, 90 + 141 (4.8 and 5.0 TB/s).
 #include <algorithm>
 
 #include "dmt_internal.h"
@@ -819,6 +819,10 @@ __global__ __launch_bounds__(256) void sequence_rows(const int64_t* offsets, int
 
 constexpr int64_t kMost = 1ll << 30;          // rows and sequences: a tile past the last row is still a 32-bit row
 
+// Longer equal sequences are whole too where that leaves kWhole waves: bfloat16, forward and backward, 2048 of 128 x 256 93 + 145 us (2048 waves), cut
+// 42 + 82 + 36 + 138; 256 of 256 x 1024 126 + 195 (1024 waves), cut 66 + 82 + 51 + 140; 128 of 512 x 1024 220 + 345 (512), cut 78 + 83 + 58 + 138.
+constexpr int64_t kWhole = 1024;
+
 // Waves that fill the chip with enough rows requested at once; stretches are as long as leaves so many, since a longer one is more
 // often whole sequences, and then the first launch has nothing to read.  Equal sequences of up to kSub rows are always a walker's, one or some:
 // 4096 of 64 x 64 bfloat16, forward and backward, 37 + 53 us, cut in four 49 + 68; one of 50 x 128 alone 13, in seven of eight rows 8.3 us.  131072 x 256 bfloat16 in 4096 ragged sequences: stretches of 32
@@ -835,7 +839,7 @@ Cut cut_of(int64_t rows, int64_t cols, int elem_bytes, bool dense, int64_t seque
   auto waves = [&](int64_t sub) { return (rows + sub - 1) / sub * c.tiles * c.group / 64; };
   const int64_t length = dense && rows > 0 ? rows / sequences : kSub + 1;
   const bool few = rows <= walkers * kSub;                 // one chunk holds all
-  c.whole = length <= (few ? 2 * kTile : kSub);
+  c.whole = dense && rows > 0 && (length <= (few ? 2 * kTile : kSub) || waves(length) >= kWhole);
   if (c.whole) {
     c.sub = length * std::max<int64_t>(1, 2 * kTile / length);
   } else if (few) {

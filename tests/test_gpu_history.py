@@ -135,7 +135,8 @@ def test_gated_scan(dmt, rows, cols, sequences, pad, shift, kind, dtype, gd):
 
 
 @pytest.mark.parametrize("rows,cols,sequences,dtype", [(70_000, 130, 10_000, "bf16"), (66_000, 128, 66_000, "f16"),
-                                                       (105_000, 64, 2_100, "f32"), (68_000, 300, 4_000, "f32")])
+                                                       (105_000, 64, 2_100, "f32"), (68_000, 300, 4_000, "f32"),
+                                                       (21_840, 1_100, 312, "f32"), (27_300, 3_600, 300, "bf16")])
 def test_gated_scan_of_many_equal_sequences(dmt, rows, cols, sequences, dtype):
     scan_case(dmt, rows, cols, sequences, 0, 0, dtype, dtype, "equal", False, True)
 
