@@ -149,6 +149,13 @@ def test_gated_scan_of_padded_rooms(dmt, room, cols, sequences, dtype, kind):
     scan_case(dmt, room * sequences, cols, sequences, 0, 0, dtype, dtype, kind, False, True, seed=room)
 
 
+@pytest.mark.parametrize("kind", ["room", "ragged"])
+@pytest.mark.parametrize("room,cols,sequences,dtype", [(33, 230, 1100, "f32"), (50, 520, 400, "bf16"), (61, 129, 1050, "f32")])
+def test_gated_scan_of_many_padded_rooms(dmt, room, cols, sequences, dtype, kind):
+    """So many that stretches are as long as the rooms; the workspace is of just the size asked for."""
+    scan_case(dmt, room * sequences, cols, sequences, 0, 0, dtype, dtype, kind, False, True, seed=room)
+
+
 @pytest.mark.parametrize("rows,cols,starts", [(400_000, 64, [0]), (400_000, 64, [0, 131, 399_990]), (300_000, 5, [0, 250_000]),
                                               (1_100_000, 20, [0, 1_000_003])])
 def test_gated_scan_of_long_sequences(dmt, rows, cols, starts):
