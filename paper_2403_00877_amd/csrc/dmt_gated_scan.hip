@@ -156,10 +156,11 @@ __device__ __forceinline__ void report_bad(const Scan& a, int lo, int hi, int at
 // f = sigmoid(x) and 1 - f from e = exp(-x): f = 1 / (1 + e), 1 - f = e f.  The product x log2 e is rounded, so e is off by up to 1.25 |x|
 // units of 2^-24 and two more; f and 1 - f then by f (1 - f) times that, at most 0.35 units, and by a few units of their own.  The reciprocal
 // gives 0 where its result is below 2^-126, so f is 0 from e = 2^126 on, and e f with it: 1 - f is taken as 1 where it is that to half a unit, from 2^25 on.
+// A NaN is in f and in 1 - f (the comparison is false; a minimum would take the number).
 __device__ __forceinline__ float exp_minus(float x) { return __builtin_amdgcn_exp2f(x * -1.44269504088896341f); }
 __device__ __forceinline__ void from_exp(float e, float& f, float& rest) {
   f = __builtin_amdgcn_rcpf(1.f + e);
-  rest = e >= 0x1p25f ? 1.f : __builtin_fminf(e * f, 1.f);
+  rest = e >= 0x1p25f ? 1.f : e * f;
 }
 __device__ __forceinline__ void sigmoids(float x, float& f, float& rest) { from_exp(exp_minus(x), f, rest); }
 
