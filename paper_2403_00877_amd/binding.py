@@ -799,6 +799,7 @@ def dmt_expert_combine_bwd(dy: torch.Tensor, z: Optional[torch.Tensor], slot: to
                            dz: Optional[torch.Tensor] = None, dweights: Optional[torch.Tensor] = None,
                            stream=None) -> None:
     """dz[slot[i][j]] = weights[i][j] * dy[i], zeros elsewhere; dweights[i][j] = dy[i] . z[slot[i][j]]."""
+    assert dweights is None or z is not None, "dweights: of z"
     at, n, k = _slots(slot)
     cols = dy.shape[1]
     on = _here(stream, dy, z, slot, source, weights, dz, dweights)
