@@ -684,12 +684,19 @@ def dmt_gated_scan_kept_bytes(rows: int, cols: int) -> int:
     return int(_lib.dmt_gated_scan_kept_bytes(rows, cols))
 
 
+def _sequences(sequences: Optional[int], sequence_of: Optional[torch.Tensor]) -> int:
+    """How many there are: one unless said; with ids it has to be said (rows of ids past the last would be of no sequence)."""
+    assert sequences is not None or sequence_of is None, "sequences: how many sequence_of names"
+    return 1 if sequences is None else sequences
+
+
 def dmt_gated_scan_fwd(gate: torch.Tensor, value: torch.Tensor, h: torch.Tensor, workspace: Optional[torch.Tensor],
-                       form: str = "coupled", sequence_of: Optional[torch.Tensor] = None, sequences: int = 1,
+                       form: str = "coupled", sequence_of: Optional[torch.Tensor] = None, sequences: Optional[int] = None,
                        initial: Optional[torch.Tensor] = None, final: Optional[torch.Tensor] = None,
                        kept: Optional[torch.Tensor] = None, first_bad: Optional[torch.Tensor] = None, stream=None) -> None:
     """h_t = f h_{t-1} + (1 - f) value_t (form "free": + value_t), f = sigmoid(gate_t), along the rows of each sequence."""
     rows, cols = gate.shape
+    sequences = _sequences(sequences, sequence_of)
     on = _here(stream, gate, value, h, workspace, sequence_of, initial, final, kept, first_bad)
     f32, states = torch.float32, sequences * cols
     _check("dmt_gated_scan_fwd", _lib.dmt_gated_scan_fwd(
@@ -701,11 +708,12 @@ def dmt_gated_scan_fwd(gate: torch.Tensor, value: torch.Tensor, h: torch.Tensor,
 
 def dmt_gated_scan_bwd(gate: torch.Tensor, value: torch.Tensor, dh: torch.Tensor, dgate: torch.Tensor,
                        dvalue: torch.Tensor, kept: torch.Tensor, workspace: Optional[torch.Tensor], form: str = "coupled",
-                       sequence_of: Optional[torch.Tensor] = None, sequences: int = 1,
+                       sequence_of: Optional[torch.Tensor] = None, sequences: Optional[int] = None,
                        initial: Optional[torch.Tensor] = None, dfinal: Optional[torch.Tensor] = None,
                        dinitial: Optional[torch.Tensor] = None, stream=None) -> None:
     """Gradients of gate, value and initial from those of h and final; kept as the forward left it."""
     rows, cols = gate.shape
+    sequences = _sequences(sequences, sequence_of)
     on = _here(stream, gate, value, dh, dgate, dvalue, kept, workspace, sequence_of, initial, dfinal, dinitial)
     f32, states = torch.float32, sequences * cols
     _check("dmt_gated_scan_bwd", _lib.dmt_gated_scan_bwd(
