@@ -639,7 +639,7 @@ dmt_status dmt_grad_clip(const dmt_grad_tensor* tensors, int64_t count, float ma
  * one after another (a sequence may have none).  A row with a negative id belongs to none: it takes no part, its outputs are
  * zeros, and its inputs may hold anything.  So may one with an id >= sequences, which first_bad reports.  NULL: `sequences` sequences of
  * rows / sequences rows each.  Rows of one id with others between them are that many pieces, each a sequence
- * from the id's initial state on; which of them the id's row of a per-sequence output holds is not said.
+ * from the id's initial state on; which of them a channel of the id's row of a per-sequence output is from is not said.
  */
 
 /*
@@ -662,10 +662,13 @@ typedef enum {
  *   h_t = f_t h_{t-1} + u_t,   u as `form` says,   h before the first row = initial[sequence] (NULL: 0)
  *   gate, value, h   [rows][cols] of dtype
  *   initial, final   float32 [sequences][cols]; final: the state after the last row; rows of sequences without rows are
- *                    not written; either may be NULL; they must not overlap
+ *                    not written (where a state is to pass over them, final holds a copy of initial before the call); either may be
+ *                    NULL; they must not overlap
  *   kept             what dmt_gated_scan_bwd reads, of dmt_gated_scan_kept_bytes(rows, cols) bytes, 256-byte aligned; NULL: nothing is kept
  *   workspace        of dmt_gated_scan_workspace_bytes(rows, cols), for the forward as for the backward
- * States are float32 whatever dtype is; only h is rounded.  A NaN or an infinity stays in its sequence and channel.
+ * States are float32 whatever dtype is; only h is rounded.  A NaN or an infinity stays in its sequence and channel, where a NaN gate makes
+ * NaN of f and of 1 - f, and what an infinite state leads to is an infinity or NaN.  An f or a 1 - f below 2^-126 may be 0; of
+ * a gate far from 0 the smaller one of the two is off by up to 1.25 |gate| 2^-24 of itself.
  * cols >= 1, rows >= 0, sequences >= 0; without sequence_of DMT_EINVAL unless sequences divides rows.  DMT_ENOTSUP for
  * rows or sequences beyond 2^30, cols beyond 2^24.
  */

@@ -12,9 +12,11 @@
 // The backward needs h_{t-1}: the forward keeps the state in front of every 8th row in float32, from which a walker goes through
 // its 8 rows again, so neither h nor a rounded h is read.
 //
-// Bound by memory where sequences are long: two of 65536 x 512 bfloat16, forward 80 + 87 us (the rows are read twice, 268 MB each time,
-// and 168 MB written), backward 64 + 139 (688 MB in the second launch, 4.9 TB/s).  4096 ragged ones, 131072 x 256 bfloat16, 21 + 50 us.  2048 padded
-// ones, 102400 x 201 float32, forward 6 + 50 us, backward 5 + 68.  4096 of 64 x 256 bfloat16 whole, one launch each, 90 + 141 (4.8 and 5.0 TB/s).
+// Bound by memory where sequences are long: two of 65536 x 512 bfloat16, forward 80 + 86 us (the rows are read twice, 268 MB each time,
+// and 168 MB written), backward 65 + 141 (705 MB in the second launch, 5.0 TB/s).  4096 ragged ones, 131072 x 256 bfloat16, forward 22 + 51 us, backward
+// 25 + 94.  2048 padded ones, 102400 x 201 float32, forward 6 + 51 us, backward 5 + 69.  4096 of 64 x 256 bfloat16 whole, one launch each, 90 + 141 (4.8 and
+// 5.0 TB/s).  A later chunk looks through the maps of all earlier ones of its sequence: (chunks)^2 / 2 of 8 bytes a channel.  2^18 rows of 512 bfloat16 as one
+// sequence for 16: second launches 192 + 300 us for 185 + 284; 2^20 as one for 64: 938 + 1366 for 743 + 1203; 2^24 of 16 channels as one for 256: 491 + 940 for 411 + 851.
 #include <algorithm>
 
 #include "dmt_internal.h"
@@ -154,7 +156,7 @@ __device__ __forceinline__ void report_bad(const Scan& a, int lo, int hi, int at
 }
 
 // f = sigmoid(x) and 1 - f from e = exp(-x): f = 1 / (1 + e), 1 - f = e f.  The product x log2 e is rounded, so e is off by up to 1.25 |x|
-// units of 2^-24 and two more; f and 1 - f then by f (1 - f) times that, at most 0.35 units, and by a few units of their own.  The reciprocal
+// units of 2^-24 and two more; f and 1 - f then by f (1 - f) times that, at most 0.65 units, and by a few units of their own.  The reciprocal
 // gives 0 where its result is below 2^-126, so f is 0 from e = 2^126 on, and e f with it: 1 - f is taken as 1 where it is that to half a unit, from 2^25 on.
 // A NaN is in f and in 1 - f (the comparison is false; a minimum would take the number).
 __device__ __forceinline__ float exp_minus(float x) { return __builtin_amdgcn_exp2f(x * -1.44269504088896341f); }
@@ -848,8 +850,10 @@ Cut cut_of(int64_t rows, int64_t cols, int elem_bytes, bool dense, int64_t seque
   } else {
     c.sub = kSub;
     while (c.sub > 2 * kTile && waves(c.sub) < waves_for(elem_bytes)) c.sub /= 2;
-    // rooms of a padded batch begin where stretches of their length do: 2048 of 50 x 201 float32 56 + 74 us for 69 + 92; where that leaves few
-    // waves, and the rows are ragged, it costs (262144 x 16 bfloat16 in 4096 sequences, 512 waves: 91 + 131 for 40 + 52)
+    // rooms of a padded batch begin where stretches of their length do, forward + backward on one state, half of the rooms' rows there: 2048 of 50 x 201 float32 36 +
+    // 68 us for 45 + 92, 1024 of 64 x 256 bfloat16 32 + 48 for 39 + 61, 4096 of 50 56 + 105 for 82 + 147.  A ragged batch whose mean length is such a whole number cannot be
+    // told from it: 4096 of 50 on average 106 + 167 for 118 + 194, 1400 61 + 86 for 57 + 88, but 1024 of 64, the fewest waves that are let, 68 + 103 for 44 + 67;
+    // with fewer still it costs more (262144 x 16 bfloat16 in 4096 ragged sequences, 512 waves: 91 + 131 for 40 + 52)
     const int64_t room = !dense && sequences > 0 && rows % sequences == 0 ? rows / sequences : 0;
     if (room >= kRoom && room <= kSub && waves(room) >= 1024) c.sub = room;
   }
